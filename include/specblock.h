@@ -540,6 +540,168 @@ int sb_profile(sb_ctx* ctx, int32_t enable);
 int sb_profile_read(sb_ctx* ctx, sb_kernel_stat* out);
 int sb_profile_read_gemm(sb_ctx* ctx, sb_gemm_stat* out);
 
+/* ---- 8-bit K/V cache ----------------------------------------------------
+ *
+ * A target cache that holds every value as an e4m3 code (OCP: 4 exponent and 3
+ * mantissa bits, largest 448, no infinities) times a power of two per page of
+ * 16 entries, KV head and K / V: half the bytes of a bf16 cache, for longer
+ * and more sequences (App. A.5 keeps the committed prefix on the device).
+ * The calls of this part down to sb_pool_compact need no context: they take
+ * the cache's shape, and their errors are in sb_last_error(NULL).  Page-table
+ * entries are clamped as everywhere (see sb_set_debug); lengths, row offsets
+ * and positions read on the device are cut to what the caller's buffers hold. */
+typedef struct sb_cache_shape {
+  int32_t n_heads, n_kv_heads;   /* multiple of n_kv_heads, <= 64             */
+  int32_t head_dim;              /* 64 or 128                                 */
+  int32_t dtype;                 /* elem of queries, outputs and segments     */
+  int32_t max_seqs;              /* page-table rows, 1..64                    */
+  int32_t max_pages;             /* page-table row length, 1..16384           */
+} sb_cache_shape;
+
+/* Entry i of sequence s is slot i % 16 of page page_table[s][i / 16].  Codes
+ * of a page and KV head, 16 head_dim bytes:
+ *   k: [16][head_dim]
+ *   v: [4][16][head_dim / 16][4]: slot 4 a + d, column 16 c + r at [a][r][c][d]
+ * The value is code * 2^(exp - 127), exp the page's byte (1..254). */
+typedef struct sb_kvq {
+  uint8_t* k;                  /* [n_layers][n_pages][n_kv_heads][16 head_dim] */
+  uint8_t* v;
+  uint8_t* k_exp;              /* [n_layers][n_pages][n_kv_heads]            */
+  uint8_t* v_exp;
+  const int32_t* page_table;   /* [max_seqs][max_pages]                      */
+  int32_t n_layers;            /* host value                                 */
+  int32_t n_pages;             /* host value: pages in the pool              */
+} sb_kvq;
+
+/* Entries first[s] .. last[s] - 1 of sequences s < n_seqs, all layers, from an
+ * elem cache (written by sb_prefill, say) into an 8-bit one, each through its
+ * own page table.  first, last: device [n_seqs]; max_entries: host bound of
+ * last - first (entries past first + max_entries are not stored; entries
+ * outside the page table neither).
+ * Per page, KV head and K / V: e = the least integer >= -126 with
+ * |x| <= 448 * 2^e for every finite value x stored by this call; when the page
+ * holds earlier entries (below first) its exponent does not fall, and where it
+ * rises the held codes are rounded again to the new one (exactly, but for
+ * values below the least normal code).  A code is x * 2^-e rounded to nearest,
+ * ties to even; infinities and NaN become NaN.  Other slots keep their bytes.
+ * Sequences must not share the pages written.  The layer counts must agree.
+ * Errors: SB_EINVAL, SB_ESHAPE, SB_EDTYPE, SB_EHIP. */
+int sb_kvq_store(const sb_cache_shape* shape, int32_t n_seqs, const sb_kv* src,
+                 const int32_t* first, const int32_t* last,
+                 int32_t max_entries, sb_kvq* dst, void* stream);
+
+/* Rows of an attention call: rows row_off[s] .. row_off[s + 1] - 1 belong to
+ * sequence s.  A row sees the prefix entries of its sequence (within the
+ * window, below) and the segment slots j < seg_len[s] whose bit j % 32 of
+ * vis[row][j / 32] is set.  All pointers are device pointers. */
+typedef struct sb_attn_rows {
+  int32_t n_seqs;              /* host, 1..max_seqs                          */
+  int32_t n_rows;              /* host: rows of q, out, pos and vis          */
+  int32_t rows_per_seq;        /* host: most rows of one sequence, 1..65535;
+                                  rows of a sequence past it are not computed */
+  int32_t max_prefix;          /* host bound of prefix_len; 0: the page
+                                  table's capacity.  Entries past it are not
+                                  seen                                       */
+  int32_t vis_words;           /* host: words per row of vis, 0..16          */
+  int32_t seg_pages;           /* host: segment pages per sequence; 0: none  */
+  const int32_t* row_off;      /* [n_seqs + 1], ascending                    */
+  const int32_t* pos;          /* [n_rows] positions (NULL without a window) */
+  const int32_t* prefix_len;   /* [n_seqs] entries in the cache              */
+  const int32_t* seg_len;      /* [n_seqs]                                   */
+  const uint32_t* vis;         /* [n_rows][vis_words]                        */
+  const void* seg_k;           /* elem [n_seqs][seg_pages][n_kv_heads][16][hd] */
+  const void* seg_v;           /* elem [n_seqs][seg_pages][n_kv_heads][hd][16] */
+} sb_attn_rows;
+
+/* Workspace bytes of sb_kvq_attend for these host values (the device pointers
+ * are not looked at; 0 if they are invalid). */
+size_t sb_kvq_attend_workspace(const sb_cache_shape* shape,
+                               const sb_attn_rows* rows, int32_t window,
+                               int32_t sinks);
+
+/* Tree attention over one layer of an 8-bit cache (the masked attention of
+ * Sec. 3.2 and App. A.2; a single token is a tree of one node):
+ *   out[i][h] = sum_e softmax_e(q[i][h] . k_e / sqrt(head_dim)) v_e
+ * over the entries and segment slots that row i sees, KV head h / (n_heads /
+ * n_kv_heads).  A row that sees nothing gives zeros; hidden entries add
+ * nothing, whatever they hold.  window > 0: row i sees entry e only when
+ * e < sinks or e > pos[i] - window (its own window and the first `sinks`
+ * entries, which stay visible); the segment is not windowed.  window 0: the
+ * whole prefix.
+ * q, out: elem [n_rows][n_heads][head_dim], 16-byte aligned, not overlapping;
+ * rows outside row_off's range are left as they were.
+ * workspace: device, 256-byte aligned, of sb_kvq_attend_workspace bytes, used
+ * until the call's work has run; calls (and captured graphs) that may run at
+ * the same time need one each.
+ * Errors: SB_EINVAL, SB_ESHAPE, SB_EDTYPE, SB_EBUDGET (workspace), SB_EHIP. */
+int sb_kvq_attend(const sb_cache_shape* shape, const sb_kvq* kv, int32_t layer,
+                  const sb_attn_rows* rows, const void* q, int32_t window,
+                  int32_t sinks, void* out, void* workspace,
+                  size_t workspace_bytes, void* stream);
+
+/* sb_tree_verify and sb_commit over an 8-bit target cache.  Verification
+ * attends as sb_kvq_attend does, with the tree's nodes as rows and segment
+ * (window and sinks as there, 0 and 0 for the whole prefix); the commit stores
+ * the accepted entries as sb_kvq_store does.  The drafter's cache stays in the
+ * element type.  Errors: as sb_tree_verify and sb_commit. */
+int sb_tree_verify_kvq(sb_ctx* ctx, const sb_seqs* seqs, const sb_tree* tree,
+                       const sb_kvq* target_kv, int32_t window, int32_t sinks,
+                       sb_verify_out* out, void* stream);
+int sb_commit_kvq(sb_ctx* ctx, sb_seqs* seqs, const sb_tree* tree,
+                  const sb_verify_out* verify, const sb_accept_out* acc,
+                  sb_kvq* target_kv, sb_kv* draft_kv, void* stream);
+
+/* ---- page pool ----------------------------------------------------------
+ *
+ * Pages that sequences take, share, return and move.  One pool serves the
+ * caches that go through one page table (a target's and its drafter's, say).
+ * A page is free when no sequence holds it.  All state is on the device; the
+ * calls run on the stream one after the other, never wait for the host, and
+ * give the same pages whenever they are repeated from the same state. */
+typedef struct sb_pool {
+  int32_t* page_table;   /* [max_seqs][max_pages]; entries < held[s] count   */
+  int32_t* held;         /* [max_seqs] pages that sequence s holds           */
+  int32_t* refs;         /* [n_pages] sequences that hold the page           */
+  int32_t* refused;      /* [1] requests that found no page or no table room */
+  int32_t* scratch;      /* [sb_pool_scratch_ints(n_pages)]                  */
+  int32_t n_pages;       /* host, 1 .. 2^20                                  */
+} sb_pool;
+
+/* int32 values of sb_pool.scratch (0 if n_pages is invalid). */
+size_t sb_pool_scratch_ints(int32_t n_pages);
+
+/* Every page free, no sequence holding any, tables and refused 0. */
+int sb_pool_reset(const sb_cache_shape* shape, const sb_pool* pool,
+                  void* stream);
+/* Sequences s < n_seqs come to hold ceil((len[s] + extra) / 16) pages (len:
+ * device [n_seqs]; those that hold as many already are left), in order of s
+ * the lowest free pages.  Where the pool or the table row runs out a sequence
+ * holds what there was and refused counts it. */
+int sb_pool_grow(const sb_cache_shape* shape, const sb_pool* pool,
+                 int32_t n_seqs, const int32_t* len, int32_t extra,
+                 void* stream);
+/* The listed sequences (host [n], distinct) return what they hold. */
+int sb_pool_release(const sb_cache_shape* shape, const sb_pool* pool, int32_t n,
+                    const int32_t* seqs, void* stream);
+/* child[i] becomes a continuation of parent[i] (host [n]; children distinct,
+ * no child a parent): it returns what it holds, then shares the parent's full
+ * pages below len[parent] (device [max_seqs], cut to what the parent holds)
+ * and gets a copy of its last, partly filled one in the lowest free page (in
+ * order of i; refused counts a child that finds none: it holds the full pages
+ * only).  kv, kvq: the caches whose pages are copied (either may be NULL),
+ * with the pool's page table and page count. */
+int sb_pool_fork(const sb_cache_shape* shape, const sb_pool* pool, int32_t n,
+                 const int32_t* parent, const int32_t* child,
+                 const int32_t* len, const sb_kv* kv, const sb_kvq* kvq,
+                 void* stream);
+/* Moves the pages in use to the front of the pool: with n in use, those at or
+ * above n, in ascending order, to the free ones below n, in ascending order;
+ * tables and refs follow.  The bytes of pages that became free stay. */
+int sb_pool_compact(const sb_cache_shape* shape, const sb_pool* pool,
+                    const sb_kv* kv, const sb_kvq* kvq, void* stream);
+/* Errors of the pool's calls: SB_EINVAL (NULL, misaligned, lists out of range
+ * or not distinct, another page table), SB_ESHAPE, SB_EDTYPE, SB_EHIP. */
+
 #ifdef __cplusplus
 }
 #endif

@@ -72,6 +72,28 @@ class KV(C.Structure):
                 ("n_pages", i32)]
 
 
+class CacheShape(C.Structure):
+    _fields_ = [("n_heads", i32), ("n_kv_heads", i32), ("head_dim", i32),
+                ("dtype", i32), ("max_seqs", i32), ("max_pages", i32)]
+
+
+class KVQ(C.Structure):
+    _fields_ = [("k", vp), ("v", vp), ("k_exp", vp), ("v_exp", vp),
+                ("page_table", vp), ("n_layers", i32), ("n_pages", i32)]
+
+
+class AttnRows(C.Structure):
+    _fields_ = [("n_seqs", i32), ("n_rows", i32), ("rows_per_seq", i32),
+                ("max_prefix", i32), ("vis_words", i32), ("seg_pages", i32),
+                ("row_off", vp), ("pos", vp), ("prefix_len", vp),
+                ("seg_len", vp), ("vis", vp), ("seg_k", vp), ("seg_v", vp)]
+
+
+class Pool(C.Structure):
+    _fields_ = [("page_table", vp), ("held", vp), ("refs", vp),
+                ("refused", vp), ("scratch", vp), ("n_pages", i32)]
+
+
 class Seqs(C.Structure):
     _fields_ = [("n_seqs", i32), ("root", vp), ("T", vp), ("cond_taps", vp)]
 
@@ -124,7 +146,10 @@ EXPORTS = ["sb_row_capacity", "sb_workspace_bytes",
            "sb_pack_weight",
            "sb_set_bucket_override", "sb_accept_sample", "sb_adapt_push",
            "sb_head_update", "sb_accept_sample_noalloc", "sb_set_debug",
-           "sb_device_check"]
+           "sb_device_check", "sb_kvq_store", "sb_kvq_attend_workspace",
+           "sb_kvq_attend", "sb_tree_verify_kvq", "sb_commit_kvq",
+           "sb_pool_scratch_ints", "sb_pool_reset", "sb_pool_grow",
+           "sb_pool_release", "sb_pool_fork", "sb_pool_compact"]
 
 _lib = None
 
@@ -195,6 +220,33 @@ def load(path: str = LIB_PATH):
     lib.sb_profile_read.restype = C.c_int
     lib.sb_profile_read_gemm.argtypes = [vp, P(GemmStat)]
     lib.sb_profile_read_gemm.restype = C.c_int
+    S = P(CacheShape)
+    lib.sb_kvq_store.argtypes = [S, i32, P(KV), vp, vp, i32, P(KVQ), vp]
+    lib.sb_kvq_store.restype = C.c_int
+    lib.sb_kvq_attend_workspace.argtypes = [S, P(AttnRows), i32, i32]
+    lib.sb_kvq_attend_workspace.restype = C.c_size_t
+    lib.sb_kvq_attend.argtypes = [S, P(KVQ), i32, P(AttnRows), vp, i32, i32,
+                                  vp, vp, C.c_size_t, vp]
+    lib.sb_kvq_attend.restype = C.c_int
+    lib.sb_tree_verify_kvq.argtypes = [vp, P(Seqs), P(Tree), P(KVQ), i32, i32,
+                                       P(VerifyOut), vp]
+    lib.sb_tree_verify_kvq.restype = C.c_int
+    lib.sb_commit_kvq.argtypes = [vp, P(Seqs), P(Tree), P(VerifyOut),
+                                  P(AcceptOut), P(KVQ), P(KV), vp]
+    lib.sb_commit_kvq.restype = C.c_int
+    lib.sb_pool_scratch_ints.argtypes = [i32]
+    lib.sb_pool_scratch_ints.restype = C.c_size_t
+    lib.sb_pool_reset.argtypes = [S, P(Pool), vp]
+    lib.sb_pool_reset.restype = C.c_int
+    lib.sb_pool_grow.argtypes = [S, P(Pool), i32, vp, i32, vp]
+    lib.sb_pool_grow.restype = C.c_int
+    lib.sb_pool_release.argtypes = [S, P(Pool), i32, P(i32), vp]
+    lib.sb_pool_release.restype = C.c_int
+    lib.sb_pool_fork.argtypes = [S, P(Pool), i32, P(i32), P(i32), vp, P(KV),
+                                 P(KVQ), vp]
+    lib.sb_pool_fork.restype = C.c_int
+    lib.sb_pool_compact.argtypes = [S, P(Pool), P(KV), P(KVQ), vp]
+    lib.sb_pool_compact.restype = C.c_int
     _lib = lib
     return lib
 

@@ -17,6 +17,7 @@ BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libspecblock.so")
 SOURCES = ["gemm.hip", "elementwise.hip", "attention.hip", "vocab.hip",
            "tree.hip", "sampling.hip", "adapt.hip",
+           "kvq_attn.hip", "kvq_store.hip", "pool.hip", "kvcache.hip",
            "engine.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++17",

@@ -1055,13 +1055,19 @@ void attn_time_next_launch(hipEvent_t start, hipEvent_t stop) {
 
 bool attn_time_pending() { return g_attn_start != nullptr; }
 
+void attn_take_events(hipEvent_t* start, hipEvent_t* stop) {
+  *start = g_attn_start;
+  *stop = g_attn_stop;
+  g_attn_start = g_attn_stop = nullptr;
+}
+
 template <typename T>
 void launch_tree_attn(const T* q, const CallPlan& p, const KVView& kv,
                       int rows_per_seq_cap, int H, int Hkv, int hd,
                       int n_split, int max_prefix, float* o_part, float* ml,
                       T* out, int max_split, int* split_rows, hipStream_t st) {
-  hipEvent_t ea = g_attn_start, eb = g_attn_stop;
-  g_attn_start = g_attn_stop = nullptr;
+  hipEvent_t ea, eb;
+  attn_take_events(&ea, &eb);
   // with a merge, the kernel carries the start event and the merge the stop
   hipEvent_t ka = ea, kb = n_split > 1 ? nullptr : eb;
   AttnShape a =

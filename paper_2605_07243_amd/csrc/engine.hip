@@ -10,6 +10,7 @@
 #include <vector>
 
 #include "kernels.h"
+#include "kvq.h"
 #include "specblock.h"
 
 using namespace sb;
@@ -226,6 +227,15 @@ static int fail(sb_ctx* c, int code, const std::string& msg) {
     c->err = msg;
   else
     g_create_err = msg;
+  return code;
+}
+
+int sb::fail_global(int code, const char* msg) noexcept {
+  try {
+    g_create_err = msg;
+  } catch (...) {   // (no memory for the message: the code stands alone)
+    g_create_err.clear();
+  }
   return code;
 }
 
@@ -751,6 +761,9 @@ struct Prefix {
   void* seg_v;
   int seg_pages;
   int max_keys = 0;   // prefill passes: the most keys a piece attends to
+  // the committed prefix in 8 bits instead (kv is null), its window and sinks
+  const sb_kvq* kvq = nullptr;
+  int window = 0, sinks = 0;
 };
 
 // Decoder layer body after the attention-norm operand is in A: QKV + RoPE,
@@ -770,11 +783,13 @@ void layer_body(sb_ctx* c, const sb_layer_weights& lw, int layer,
   T* segk = static_cast<T*>(pf.seg_k) + (size_t)layer * D.S * pf.seg_pages * page;
   T* segv = static_cast<T*>(pf.seg_v) + (size_t)layer * D.S * pf.seg_pages * page;
   KVView kv{};
-  kv.k = static_cast<T*>(pf.kv->k) + (size_t)layer * pf.kv->n_pages * page;
-  kv.v = static_cast<T*>(pf.kv->v) + (size_t)layer * pf.kv->n_pages * page;
-  kv.page_table = pf.kv->page_table;
+  if (pf.kv != nullptr) {   // (verification over an 8-bit cache has none)
+    kv.k = static_cast<T*>(pf.kv->k) + (size_t)layer * pf.kv->n_pages * page;
+    kv.v = static_cast<T*>(pf.kv->v) + (size_t)layer * pf.kv->n_pages * page;
+    kv.page_table = pf.kv->page_table;
+    kv.n_pages = pf.kv->n_pages;
+  }
   kv.max_pages = c->cfg.max_pages;
-  kv.n_pages = pf.kv->n_pages;
   kv.err = c->dbg();
   kv.seg_k = segk;
   kv.seg_v = segv;
@@ -788,23 +803,40 @@ void layer_body(sb_ctx* c, const sb_layer_weights& lw, int layer,
   const int max_prefix = causal ? pf.max_keys
                          : c->T_bound > 0 ? std::min(c->T_bound, cap_tokens)
                                           : cap_tokens;
-  const int G = D.H / D.Hkv, seq_heads = p.n_seqs * D.Hkv;
-  const int groups = attn_qgroups(rows_per_seq, G, seq_heads, D.es) * seq_heads;
-  // enough workgroups for the chip, splits of at least 128 keys (shorter
-  // ones measured slower)
-  int n_split = std::max(
-      1, ceil_div(attn_workgroup_target(rows_per_seq, G, seq_heads, D.es), groups));
-  n_split = std::min(n_split, std::max(1, max_prefix / 128));
-  if (causal) n_split = std::min<int>(n_split, std::max<size_t>(1, D.o_rows / R));
-  // a split spans at most 1024 pages of 16 keys
-  n_split = std::max(n_split, ceil_div(max_prefix, 1024 * 16));
-  n_split = std::min(n_split, D.n_split);
-  // (a prefill pass's splits are fixed: its pieces differ in length by far)
-  {
+  if (pf.kvq != nullptr) {
+    const size_t at = (size_t)layer * pf.kvq->n_pages;
+    const QView qv{pf.kvq->k + at * page, pf.kvq->v + at * page,
+                   pf.kvq->k_exp + at * D.Hkv, pf.kvq->v_exp + at * D.Hkv,
+                   pf.kvq->page_table, c->cfg.max_pages, pf.kvq->n_pages,
+                   segk, segv, pf.seg_pages, c->dbg()};
+    const QRows qr{p.seq_off, p.pos, p.prefix_len, p.seg_len, p.vis,
+                   p.vis_words, p.n_seqs, R, rows_per_seq, max_prefix,
+                   pf.window, pf.sinks};
+    const QPlan plan =
+        kvq_attn_plan(p.n_seqs, rows_per_seq, max_prefix, pf.window, pf.sinks,
+                      D.H, D.Hkv, D.hd, D.es, D.n_split);
     ProfScope ps(c, st, SB_PROF_ATTN);
-    launch_tree_attn<T>(static_cast<const T*>(c->q), p, kv, rows_per_seq, D.H,
-                        D.Hkv, D.hd, n_split, max_prefix, c->o_part, c->ml, A,
-                        D.n_split, causal ? nullptr : c->split_rows, st);
+    launch_kvq_attn<T>(static_cast<const T*>(c->q), qr, qv, D.H, D.Hkv, D.hd,
+                       plan, c->o_part, c->ml, A, st);
+  } else {
+    const int G = D.H / D.Hkv, seq_heads = p.n_seqs * D.Hkv;
+    const int groups = attn_qgroups(rows_per_seq, G, seq_heads, D.es) * seq_heads;
+    // enough workgroups for the chip, splits of at least 128 keys (shorter
+    // ones measured slower)
+    int n_split = std::max(
+        1, ceil_div(attn_workgroup_target(rows_per_seq, G, seq_heads, D.es), groups));
+    n_split = std::min(n_split, std::max(1, max_prefix / 128));
+    if (causal) n_split = std::min<int>(n_split, std::max<size_t>(1, D.o_rows / R));
+    // a split spans at most 1024 pages of 16 keys
+    n_split = std::max(n_split, ceil_div(max_prefix, 1024 * 16));
+    n_split = std::min(n_split, D.n_split);
+    // (a prefill pass's splits are fixed: its pieces differ in length by far)
+    {
+      ProfScope ps(c, st, SB_PROF_ATTN);
+      launch_tree_attn<T>(static_cast<const T*>(c->q), p, kv, rows_per_seq, D.H,
+                          D.Hkv, D.hd, n_split, max_prefix, c->o_part, c->ml, A,
+                          D.n_split, causal ? nullptr : c->split_rows, st);
+    }
   }
   ks = gemm<T>(c, A, D.H * D.hd, lw.w_o, D.d, D.H * D.hd, p.n, R, st);
   launch_residual<T>(c->x, c->P, ks, (size_t)R * D.d, p.n, R, D.d, true,
@@ -999,14 +1031,15 @@ int draft_expand_impl(sb_ctx* c, int m, const sb_seqs* sq, const sb_kv* dkv,
 
 template <typename T>
 int verify_impl(sb_ctx* c, const sb_seqs* sq, const sb_tree* t,
-                const sb_kv* tkv, sb_verify_out* out, hipStream_t st) {
+                const sb_kv* tkv, const sb_kvq* tkvq, int window, int sinks,
+                sb_verify_out* out, hipStream_t st) {
   const Dims& D = c->D;
   const TreeDims td = tree_dims(c, sq->n_seqs);
   CallPlan p = c->plan;
   p.n_seqs = sq->n_seqs;
   p.cap = sq->n_seqs * D.budget;
   launch_plan_verify(td, *t, sq->T, p, st);
-  const Prefix pf{tkv, c->tseg_k, c->tseg_v, D.tpages};
+  const Prefix pf{tkv, c->tseg_k, c->tseg_v, D.tpages, 0, tkvq, window, sinks};
   target_forward<T>(c, p, pf, D.budget, out->taps, st);
   const int n_chunks = lm_head_reduce<T>(c, c->A, c->tw.lm_head, D.V,
                                          out->logits, p.n, p.cap, 1,
@@ -1016,25 +1049,32 @@ int verify_impl(sb_ctx* c, const sb_seqs* sq, const sb_tree* t,
     launch_verify_finalize(c->vpart, n_chunks, p.n, p.cap, p.out_row,
                            out->argmax, st);
   }
-  return hip_check(c, "sb_tree_verify");
+  return hip_check(c, tkvq ? "sb_tree_verify_kvq" : "sb_tree_verify");
 }
 
 template <typename T>
 int commit_impl(sb_ctx* c, sb_seqs* sq, const sb_tree* t,
                 const sb_verify_out* v, const sb_accept_out* acc,
-                sb_kv* tkv, sb_kv* dkv, hipStream_t st) {
+                sb_kv* tkv, sb_kvq* tkvq, sb_kv* dkv, hipStream_t st) {
   const Dims& D = c->D;
   const TreeDims td = tree_dims(c, sq->n_seqs);
   CallPlan fb = c->fb;
   fb.write_through = true;
   launch_commit_plan(td, *t, *acc, sq->T, c->ci, fb, c->taps_idx, c->n_aux,
                      st);
-  const KVPools tp{tkv->k, tkv->v, tkv->page_table, c->cfg.max_pages,
-                   tkv->n_pages, c->tseg_k, c->tseg_v, D.tpages, c->dbg()};
+  KVPools tp{};
+  if (tkvq != nullptr)
+    launch_kvq_commit<T>(static_cast<const T*>(c->tseg_k),
+                         static_cast<const T*>(c->tseg_v), D.tpages, D.S, *tkvq,
+                         c->cfg.max_pages, sq->n_seqs, c->ci.T_old, c->ci.a,
+                         acc->path, D.M * D.K, D.Hkv, D.hd, c->dbg(), st);
+  else
+    tp = KVPools{tkv->k, tkv->v, tkv->page_table, c->cfg.max_pages,
+                 tkv->n_pages, c->tseg_k, c->tseg_v, D.tpages, c->dbg()};
   const KVPools dp{dkv->k, dkv->v, dkv->page_table, c->cfg.max_pages,
                    dkv->n_pages, c->dseg_k, c->dseg_v, D.dpages, c->dbg()};
-  launch_commit_apply<T>(td, *t, *acc, c->ci, tp, D.L, dp, D.LD, D.S, D.Hkv,
-                         D.hd, *sq, v->taps, st);
+  launch_commit_apply<T>(td, *t, *acc, c->ci, tp, tkvq ? 0 : D.L, dp, D.LD, D.S,
+                         D.Hkv, D.hd, *sq, v->taps, st);
   // raised before the catch-up forward: its rows attend to the entries that
   // this commit adds
   if (c->T_bound > 0) c->T_bound += D.M * D.K + 1;
@@ -1047,7 +1087,7 @@ int commit_impl(sb_ctx* c, sb_seqs* sq, const sb_tree* t,
   fb.cap = sq->n_seqs;
   drafter_forward<T>(c, fb, c->cond_buf, pf, 1, false, st);
   set_rows_likely_empty(false);
-  return hip_check(c, "sb_commit");
+  return hip_check(c, tkvq ? "sb_commit_kvq" : "sb_commit");
 }
 
 // Prefill: the prompts, one after the other, as one stream of rows that runs
@@ -1157,6 +1197,17 @@ int check_kv(sb_ctx* c, const sb_kv* kv, int n_layers, const char* what) {
   return SB_OK;
 }
 
+int check_kvq_of(sb_ctx* c, const sb_kvq* kv) {
+  if (!kv) return fail(c, SB_EINVAL, "target_kv is NULL");
+  if (bad_ptr(kv->k, 16) || bad_ptr(kv->v, 16) || bad_ptr(kv->k_exp, 1) ||
+      bad_ptr(kv->v_exp, 1) || bad_ptr(kv->page_table, 4))
+    return fail(c, SB_EINVAL, "target_kv pointer NULL or misaligned");
+  if (kv->n_layers != c->D.L)
+    return fail(c, SB_ESHAPE, "target_kv has the wrong layer count");
+  if (kv->n_pages < 1) return fail(c, SB_EINVAL, "target_kv has no pages");
+  return SB_OK;
+}
+
 int check_tree(sb_ctx* c, const sb_tree* t) {
   if (!t) return fail(c, SB_EINVAL, "tree is NULL");
   const void* ps[] = {t->n_nodes, t->token, t->parent, t->depth, t->row,
@@ -1208,8 +1259,26 @@ int sb_tree_verify(sb_ctx* c, const sb_seqs* seqs, const sb_tree* tree,
     return fail(c, SB_EINVAL, "verify out pointer NULL or misaligned");
   if (out->logits && bad_ptr(out->logits, 16))
     return fail(c, SB_EINVAL, "out->logits misaligned");
-  return is_bf16(c) ? verify_impl<bf16_t>(c, seqs, tree, target_kv, out, S_(stream))
-                    : verify_impl<float>(c, seqs, tree, target_kv, out, S_(stream));
+  return is_bf16(c) ? verify_impl<bf16_t>(c, seqs, tree, target_kv, nullptr, 0, 0, out, S_(stream))
+                    : verify_impl<float>(c, seqs, tree, target_kv, nullptr, 0, 0, out, S_(stream));
+}
+
+int sb_tree_verify_kvq(sb_ctx* c, const sb_seqs* seqs, const sb_tree* tree,
+                       const sb_kvq* target_kv, int32_t window, int32_t sinks,
+                       sb_verify_out* out, void* stream) {
+  int rc = check_common(c);
+  if (rc) return rc;
+  if ((rc = check_seqs(c, seqs)) || (rc = check_kvq_of(c, target_kv)) ||
+      (rc = check_tree(c, tree)))
+    return rc;
+  if (window < 0 || sinks < 0)
+    return fail(c, SB_EINVAL, "window and sinks must not be negative");
+  if (!out || bad_ptr(out->argmax, 4) || bad_ptr(out->taps, 4))
+    return fail(c, SB_EINVAL, "verify out pointer NULL or misaligned");
+  if (out->logits && bad_ptr(out->logits, 16))
+    return fail(c, SB_EINVAL, "out->logits misaligned");
+  return is_bf16(c) ? verify_impl<bf16_t>(c, seqs, tree, nullptr, target_kv, window, sinks, out, S_(stream))
+                    : verify_impl<float>(c, seqs, tree, nullptr, target_kv, window, sinks, out, S_(stream));
 }
 
 }  // extern "C"
@@ -1448,8 +1517,24 @@ int sb_commit(sb_ctx* c, sb_seqs* seqs, const sb_tree* tree,
   if (!verify || bad_ptr(verify->taps, 4) || !acc || bad_ptr(acc->path, 4) ||
       bad_ptr(acc->n_accepted, 4) || bad_ptr(acc->bonus, 4))
     return fail(c, SB_EINVAL, "commit pointer NULL or misaligned");
-  return is_bf16(c) ? commit_impl<bf16_t>(c, seqs, tree, verify, acc, target_kv, draft_kv, S_(stream))
-                    : commit_impl<float>(c, seqs, tree, verify, acc, target_kv, draft_kv, S_(stream));
+  return is_bf16(c) ? commit_impl<bf16_t>(c, seqs, tree, verify, acc, target_kv, nullptr, draft_kv, S_(stream))
+                    : commit_impl<float>(c, seqs, tree, verify, acc, target_kv, nullptr, draft_kv, S_(stream));
+}
+
+int sb_commit_kvq(sb_ctx* c, sb_seqs* seqs, const sb_tree* tree,
+                  const sb_verify_out* verify, const sb_accept_out* acc,
+                  sb_kvq* target_kv, sb_kv* draft_kv, void* stream) {
+  int rc = check_common(c);
+  if (rc) return rc;
+  if ((rc = check_seqs(c, seqs)) || (rc = check_tree(c, tree)) ||
+      (rc = check_kvq_of(c, target_kv)) ||
+      (rc = check_kv(c, draft_kv, c->D.LD, "draft_kv")))
+    return rc;
+  if (!verify || bad_ptr(verify->taps, 4) || !acc || bad_ptr(acc->path, 4) ||
+      bad_ptr(acc->n_accepted, 4) || bad_ptr(acc->bonus, 4))
+    return fail(c, SB_EINVAL, "commit pointer NULL or misaligned");
+  return is_bf16(c) ? commit_impl<bf16_t>(c, seqs, tree, verify, acc, nullptr, target_kv, draft_kv, S_(stream))
+                    : commit_impl<float>(c, seqs, tree, verify, acc, nullptr, target_kv, draft_kv, S_(stream));
 }
 
 int sb_prefill(sb_ctx* c, const sb_seqs* seqs, const int32_t* prompt,

@@ -76,6 +76,8 @@ bool gemm_time_pending();
 // Kernel-attached timing of the next tree-attention call (kernel + merge).
 void attn_time_next_launch(hipEvent_t start, hipEvent_t stop);
 bool attn_time_pending();
+// The events set for the next call, which takes them (null: none).
+void attn_take_events(hipEvent_t* start, hipEvent_t* stop);
 // P[ks][m][n] = X[m] . W[n] over K-chunk ks for the first *m_count rows.
 // bf16 W is fragment-packed, f32 W row-major.  ksplit <= 0: the plan's
 // split; otherwise at most ksplit K-chunks.  Returns the K-chunks written.

@@ -1,0 +1,236 @@
+"""The 8-bit K/V cache and the page pool of libspecblock.so over torch tensors.
+
+Thin handles around the ``sb_kvq_*`` and ``sb_pool_*`` calls: they check the
+tensors they are given (type, shape, layout, device), keep them alive and
+marshal arguments; every step runs in the library's HIP kernels on the current
+stream of the tensors' device.  Nothing here waits for the device.
+"""
+from __future__ import annotations
+
+import ctypes as C
+
+import torch
+
+from . import binding as B
+
+
+def _tensor(t, name, dtype, shape, device=None):
+    """The tensor's address, after checking what the kernels rely on."""
+    if (not isinstance(t, torch.Tensor) or t.dtype != dtype
+            or tuple(t.shape) != tuple(shape) or not t.is_contiguous()):
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape "
+                         f"{tuple(shape)}")
+    if not t.is_cuda or (device is not None and t.device != device):
+        raise ValueError(f"{name} must be on the GPU of the other tensors")
+    return C.c_void_p(t.data_ptr())
+
+
+def _call(device, fn, *args):
+    """fn(*args, stream) with the tensors' device current; raises SBError."""
+    if torch.cuda.current_device() == device.index:
+        rc = fn(*args, C.c_void_p(torch.cuda.current_stream(device).cuda_stream))
+    else:
+        with torch.cuda.device(device):
+            rc = fn(*args, C.c_void_p(torch.cuda.current_stream(device).cuda_stream))
+    if rc != B.SB_OK:
+        B.check(B.load(), None, rc)
+
+
+class Shape:
+    """sb_cache_shape: heads, element type ("bf16" or "f32") and page tables."""
+
+    def __init__(self, n_heads, n_kv_heads, head_dim, dtype, max_seqs, max_pages):
+        if dtype not in ("bf16", "f32"):
+            raise ValueError('dtype must be "bf16" or "f32"')
+        self.n_heads, self.n_kv_heads, self.head_dim = n_heads, n_kv_heads, head_dim
+        self.max_seqs, self.max_pages, self.dtype = max_seqs, max_pages, dtype
+        self.elem = torch.bfloat16 if dtype == "bf16" else torch.float32
+        self.c = B.CacheShape(n_heads, n_kv_heads, head_dim,
+                              B.SB_BF16 if dtype == "bf16" else B.SB_F32,
+                              max_seqs, max_pages)
+
+
+class PagedKV:
+    """sb_kv over tensors: k [layers][pages][Hkv][16][hd], v [..][hd][16]."""
+
+    def __init__(self, shape, k, v, page_table):
+        self.shape, self.k, self.v, self.page_table = shape, k, v, page_table
+        L, n = k.shape[:2]
+        hkv, hd, dev = shape.n_kv_heads, shape.head_dim, k.device
+        self.device = dev
+        self.c = B.KV(_tensor(k, "k", shape.elem, (L, n, hkv, 16, hd)),
+                      _tensor(v, "v", shape.elem, (L, n, hkv, hd, 16), dev),
+                      _tensor(page_table, "page_table", torch.int32,
+                              (shape.max_seqs, shape.max_pages), dev), L, n)
+
+
+class QuantKV:
+    """sb_kvq over tensors: codes uint8 [layers][pages][Hkv][16 hd], scale
+    bytes uint8 [layers][pages][Hkv]."""
+
+    def __init__(self, shape, k, v, k_exp, v_exp, page_table):
+        self.lib = B.load()
+        self.shape, self.page_table = shape, page_table
+        self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
+        L, n = k.shape[:2]
+        hkv, dev = shape.n_kv_heads, k.device
+        codes = (L, n, hkv, 16 * shape.head_dim)
+        u8 = torch.uint8
+        self.device = dev
+        self.c = B.KVQ(_tensor(k, "k", u8, codes), _tensor(v, "v", u8, codes, dev),
+                       _tensor(k_exp, "k_exp", u8, (L, n, hkv), dev),
+                       _tensor(v_exp, "v_exp", u8, (L, n, hkv), dev),
+                       _tensor(page_table, "page_table", torch.int32,
+                               (shape.max_seqs, shape.max_pages), dev), L, n)
+
+    @classmethod
+    def empty(cls, shape, n_layers, n_pages, page_table):
+        """A cache of n_pages pages (codes 0, scale 1) for the page table."""
+        dev = page_table.device
+        n = (n_layers, n_pages, shape.n_kv_heads)
+        z = lambda: torch.zeros(*n, 16 * shape.head_dim, dtype=torch.uint8,  # noqa: E731
+                                device=dev)
+        e = lambda: torch.full(n, 127, dtype=torch.uint8, device=dev)  # noqa: E731
+        return cls(shape, z(), z(), e(), e(), page_table)
+
+    def store(self, src, first, last, max_entries):
+        """Entries first[s] .. last[s] - 1 of ``src`` (a PagedKV) into this
+        cache; first, last: int32 tensors [n_seqs]."""
+        n = first.shape[0]
+        if src.shape.dtype != self.shape.dtype or src.device != self.device or (
+                src.shape.n_kv_heads, src.shape.head_dim, src.shape.max_seqs,
+                src.shape.max_pages) != (self.shape.n_kv_heads, self.shape.head_dim,
+                                         self.shape.max_seqs, self.shape.max_pages):
+            raise ValueError("the caches differ in shape or device")
+        a = _tensor(first, "first", torch.int32, (n,), self.device)
+        z = _tensor(last, "last", torch.int32, (n,), self.device)
+        _call(self.device, self.lib.sb_kvq_store, self.shape.c, n, src.c, a, z,
+              int(max_entries), self.c)
+
+
+class Attention:
+    """sb_kvq_attend for one description of rows (sb_attn_rows) and one
+    workspace: ``plan(layer, q, out)`` for every layer of a forward.  A plan
+    runs on one stream at a time; captured graphs that may run at the same
+    time need a plan each."""
+
+    def __init__(self, cache, row_off, pos, prefix_len, seg_len=None, vis=None,
+                 seg_k=None, seg_v=None, *, n_rows, rows_per_seq, max_prefix=0,
+                 window=0, sinks=0):
+        sh, dev = cache.shape, cache.device
+        self.lib, self.cache, self.device = B.load(), cache, dev
+        self.n_rows, self.window, self.sinks = n_rows, window, sinks
+        n = row_off.shape[0] - 1
+        i32 = torch.int32
+        null = C.c_void_p(0)
+        words = pages = 0
+        sl = vs = sk = sv = null
+        if seg_k is not None:
+            words, pages = vis.shape[1], seg_k.shape[1]
+            hkv, hd = sh.n_kv_heads, sh.head_dim
+            sl = _tensor(seg_len, "seg_len", i32, (n,), dev)
+            vs = _tensor(vis, "vis", i32, (n_rows, words), dev)
+            sk = _tensor(seg_k, "seg_k", sh.elem, (n, pages, hkv, 16, hd), dev)
+            sv = _tensor(seg_v, "seg_v", sh.elem, (n, pages, hkv, hd, 16), dev)
+        self.rows = B.AttnRows(
+            n, n_rows, rows_per_seq, max_prefix, words, pages,
+            _tensor(row_off, "row_off", i32, (n + 1,), dev),
+            null if pos is None else _tensor(pos, "pos", i32, (n_rows,), dev),
+            _tensor(prefix_len, "prefix_len", i32, (n,), dev), sl, vs, sk, sv)
+        self._keep = (row_off, pos, prefix_len, seg_len, vis, seg_k, seg_v)
+        nbytes = self.lib.sb_kvq_attend_workspace(sh.c, self.rows, window, sinks)
+        if nbytes == 0:
+            raise B.SBError(B.SB_ESHAPE, self.lib.sb_last_error(None).decode())
+        self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+        self._ws = C.c_void_p(self.workspace.data_ptr())
+        self._rows_shape = (n_rows, sh.n_heads, sh.head_dim)
+
+    def __call__(self, layer, q, out=None):
+        """Attention outputs of the rows, [n_rows][n_heads][head_dim]."""
+        if out is None:
+            out = torch.empty_like(q)
+        el = self.cache.shape.elem
+        a = _tensor(q, "q", el, self._rows_shape, self.device)
+        o = _tensor(out, "out", el, self._rows_shape, self.device)
+        _call(self.device, self.lib.sb_kvq_attend, self.cache.shape.c, self.cache.c,
+              layer, self.rows, a, self.window, self.sinks, o, self._ws,
+              self.workspace.numel())
+        return out
+
+
+class PagePool:
+    """sb_pool over tensors, with the caches whose pages it shares and moves
+    (at most one PagedKV and one QuantKV, with the pool's page table)."""
+
+    def __init__(self, shape, page_table, held, refs, refused, caches=()):
+        self.lib, self.shape, self.device = B.load(), shape, page_table.device
+        dev, i32 = self.device, torch.int32
+        self.page_table, self.held, self.refs, self.refused = page_table, held, refs, refused
+        n = refs.shape[0]
+        ints = self.lib.sb_pool_scratch_ints(n)
+        if ints == 0:
+            raise ValueError("a pool has 1 .. 2^20 pages")
+        self.scratch = torch.empty(ints, dtype=i32, device=dev)
+        self.c = B.Pool(
+            _tensor(page_table, "page_table", i32, (shape.max_seqs, shape.max_pages)),
+            _tensor(held, "held", i32, (shape.max_seqs,), dev),
+            _tensor(refs, "refs", i32, (n,), dev),
+            _tensor(refused, "refused", i32, (1,), dev),
+            C.c_void_p(self.scratch.data_ptr()), n)
+        self.attach(caches)
+
+    @classmethod
+    def empty(cls, shape, n_pages, device="cuda"):
+        """A pool of n_pages free pages with tables of its own."""
+        z = lambda *n: torch.zeros(*n, dtype=torch.int32, device=device)  # noqa: E731
+        return cls(shape, z(shape.max_seqs, shape.max_pages), z(shape.max_seqs),
+                   z(n_pages), z(1))
+
+    def attach(self, caches):
+        """The caches that fork and compact copy from now on."""
+        kv = [c for c in caches if isinstance(c, PagedKV)]
+        kvq = [c for c in caches if isinstance(c, QuantKV)]
+        if len(kv) > 1 or len(kvq) > 1 or len(kv) + len(kvq) != len(caches):
+            raise ValueError("a pool takes at most one PagedKV and one QuantKV")
+        for c in caches:
+            if c.page_table.data_ptr() != self.page_table.data_ptr():
+                raise ValueError("the cache goes through another page table")
+            if (c.shape.n_kv_heads, c.shape.head_dim, c.shape.dtype) != (
+                    self.shape.n_kv_heads, self.shape.head_dim, self.shape.dtype):
+                raise ValueError("the cache has another shape")
+        self._caches = list(caches)
+        self._kv = kv[0].c if kv else None
+        self._kvq = kvq[0].c if kvq else None
+
+    def reset(self):
+        _call(self.device, self.lib.sb_pool_reset, self.shape.c, self.c)
+
+    def grow(self, length, extra=0):
+        """Pages for length[s] + extra entries of sequences 0 .. n - 1
+        (length: int32 tensor [n])."""
+        n = length.shape[0]
+        _call(self.device, self.lib.sb_pool_grow, self.shape.c, self.c, n,
+              _tensor(length, "length", torch.int32, (n,), self.device), int(extra))
+
+    def release(self, seqs):
+        """The listed sequences return what they hold."""
+        arr = (C.c_int32 * max(1, len(seqs)))(*seqs)
+        _call(self.device, self.lib.sb_pool_release, self.shape.c, self.c,
+              len(seqs), arr)
+
+    def fork(self, parents, children, length):
+        """children[i] continues parents[i] after length[parents[i]] entries
+        (length: int32 tensor [max_seqs])."""
+        n = len(parents)
+        if len(children) != n:
+            raise ValueError("as many children as parents")
+        pa = (C.c_int32 * max(1, n))(*parents)
+        ch = (C.c_int32 * max(1, n))(*children)
+        _call(self.device, self.lib.sb_pool_fork, self.shape.c, self.c, n, pa, ch,
+              _tensor(length, "length", torch.int32, (self.shape.max_seqs,),
+                      self.device), self._kv, self._kvq)
+
+    def compact(self):
+        """Moves the pages in use to the front of the pool."""
+        _call(self.device, self.lib.sb_pool_compact, self.shape.c, self.c,
+              self._kv, self._kvq)

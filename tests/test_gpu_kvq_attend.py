@@ -1,0 +1,358 @@
+"""Attention over the 8-bit cache (sb_kvq_attend) against float64.
+
+Tolerance, per output value, from the arithmetic (u = half a step of the
+element type, 2^-8 for bf16 and 2^-24 for fp32; A = the same weighted mean of
+|v|):
+* the output is rounded once: u |o|;
+* bf16 probabilities are rounded before the product with V, 2^-8 each: 2^-8 A;
+* a score is an fp32 sum of hd exact (bf16) or rounded products, at most
+  (hd + 4) 2^-24 of sum |q_i k_i| / sqrt(hd) off, and moves its weight by that
+  much in either direction, numerator and denominator: factor 2 on A; exp2 and
+  its argument's rounding add 2^-22 |score - reference| <= 2^-15 for scores
+  within 128 of the largest (beyond, the weights vanish);
+* fp32 sums over n keys: n 2^-24 A twice (numerator, denominator).
+"""
+import numpy as np
+import pytest
+import torch
+
+import kvq_ref as ref
+
+pytestmark = [pytest.mark.gpu, pytest.mark.timeout(300)]
+
+
+def kc():
+    from paper_2605_07243_amd import kvcache
+    return kvcache
+
+
+class Case:
+    """Random cache, tree rows and segment on the device and on the host."""
+
+    def __init__(self, dtype, H, Hkv, hd, T, rows, seed=0, window=0, sinks=0,
+                 layers=1, spare=3, max_pages=None, seg=True, rows_cap=None):
+        rng = np.random.default_rng([seed, H, hd, len(T)])
+        S = len(T)
+        self.__dict__.update(dtype=dtype, H=H, Hkv=Hkv, hd=hd, T=T, rows=rows,
+                             window=window, sinks=sinks, S=S)
+        R = max(rows)
+        mp = max_pages or (max(T) + R + 15) // 16 + 1
+        n_pages = S * mp + spare
+        shape = kc().Shape(H, Hkv, hd, dtype, S, mp)
+        self.shape = shape
+        self.table = rng.permutation(n_pages)[:S * mp].astype(np.int32).reshape(S, mp)
+        # codes of values up to 448, every finite code among them; what no
+        # sequence uses is NaN
+        def codes():
+            c = rng.integers(0, 256, (layers, n_pages, Hkv, 16 * hd)).astype(np.uint8)
+            c[(c & 127) == 127] = 0x3C
+            big = rng.random(c.shape) < 0.7      # mostly of ordinary size
+            return np.where(big, (c & 0x87) | 0x30, c).astype(np.uint8)
+        self.k, self.v = codes(), codes()
+        self.ke = rng.integers(122, 126, (layers, n_pages, Hkv)).astype(np.uint8)
+        self.ve = rng.integers(122, 126, (layers, n_pages, Hkv)).astype(np.uint8)
+        self.off = np.concatenate([[0], np.cumsum(rows)]).astype(np.int32)
+        n = int(self.off[-1])
+        self.n_rows = n
+        words, pages = (R + 31) // 32, (R + 15) // 16
+        self.vis = np.zeros((n, words), np.uint32)
+        self.pos = np.zeros(n, np.int32)
+        for s in range(S):
+            for i in range(rows[s]):
+                a = self.off[s] + i
+                self.pos[a] = T[s]
+                if i:
+                    p = self.off[s] + int(rng.integers(0, i))
+                    self.vis[a] = self.vis[p]
+                    self.pos[a] = self.pos[p] + 1
+                self.vis[a, i // 32] |= np.uint32(1 << (i % 32))
+        self.seg_len = np.array(rows, np.int32)
+        el = shape.elem
+        t = lambda a: torch.from_numpy(np.ascontiguousarray(a, np.float32)).to(el)  # noqa: E731
+        self.q_t = t(rng.standard_normal((n, H, hd)) * 0.7)
+        self.sk_t = t(rng.standard_normal((S, pages, Hkv, 16, hd)))
+        self.sv_t = t(rng.standard_normal((S, pages, Hkv, hd, 16)))
+        self.seg = seg
+
+    def plan(self, **kw):
+        d = lambda a: torch.from_numpy(np.ascontiguousarray(a)).cuda()  # noqa: E731
+        cache = kc().QuantKV(self.shape, d(self.k), d(self.v), d(self.ke), d(self.ve),
+                             d(self.table))
+        seg = dict(seg_len=d(self.seg_len), vis=d(self.vis.view(np.int32)),
+                   seg_k=self.sk_t.cuda(), seg_v=self.sv_t.cuda()) if self.seg else {}
+        args = dict(n_rows=self.n_rows, rows_per_seq=max(self.rows),
+                    max_prefix=max(self.T), window=self.window, sinks=self.sinks)
+        args.update(kw)
+        return kc().Attention(cache, d(self.off), d(self.pos),
+                              d(np.array(self.T, np.int32)), **seg, **args)
+
+    def run(self, layer=0, fill=None, **kw):
+        out = torch.full((self.n_rows, self.H, self.hd), 0.0 if fill is None else fill,
+                         dtype=self.shape.elem, device="cuda")
+        self.plan(**kw)(layer, self.q_t.cuda(), out)
+        torch.cuda.synchronize()
+        return out.float().cpu().numpy()
+
+    def sees(self, i, s):
+        e = np.arange(self.T[s])
+        see = np.ones(self.T[s], bool)
+        if self.window:
+            see = (e < self.sinks) | (e > int(self.pos[i]) - self.window)
+        n = int(self.seg_len[s]) if self.seg else 0
+        j = np.arange(n)
+        bits = ((self.vis[i, j // 32] >> (j % 32).astype(np.uint32)) & 1).astype(bool)
+        return np.concatenate([see, bits])
+
+    def check(self, got, layer=0, rows=None):
+        G, hd = self.H // self.Hkv, self.hd
+        u = 2.0 ** -8 if self.dtype == "bf16" else 2.0 ** -24
+        up = 2.0 ** -8 if self.dtype == "bf16" else 0.0
+        q = self.q_t.double().numpy()
+        worst = 0.0
+        for s in range(self.S):
+            k = ref.entries(self.k[layer], self.ke[layer], self.table[s], self.T[s], hd, False)
+            v = ref.entries(self.v[layer], self.ve[layer], self.table[s], self.T[s], hd, True)
+            n = int(self.seg_len[s]) if self.seg else 0
+            sk = self.sk_t[s].double().numpy().transpose(0, 2, 1, 3).reshape(-1, self.Hkv, hd)
+            sv = self.sv_t[s].double().numpy().transpose(0, 3, 1, 2).reshape(-1, self.Hkv, hd)
+            k = np.concatenate([k, sk[:n]])
+            v = np.concatenate([v, sv[:n]])
+            for i in range(self.off[s], self.off[s + 1]):
+                if rows is not None and i not in rows:
+                    continue
+                see = self.sees(i, s)
+                for h in range(self.H):
+                    o, a, dot = ref.attend_row(q[i, h], k[:, h // G], v[:, h // G], see)
+                    d = 2 * ((hd + 4) * 2.0 ** -24 * dot + 2.0 ** -15
+                             + see.sum() * 2.0 ** -24)
+                    tol = u * np.abs(o) + (up + d) * a + 1e-30
+                    err = np.abs(got[i, h] - o)
+                    assert (err <= tol).all(), (s, i, h, (err / tol).max())
+                    if see.any():
+                        worst = max(worst, float((err / tol).max()))
+        return worst
+
+
+SHAPES = [("bf16", 8, 2, 128), ("bf16", 8, 8, 64), ("bf16", 5, 1, 64),
+          ("bf16", 16, 2, 128), ("f32", 4, 4, 64), ("f32", 8, 2, 128)]
+
+
+@pytest.mark.parametrize("dtype,H,Hkv,hd", SHAPES)
+@pytest.mark.parametrize("T,rows", [
+    ([0], [1]), ([1], [1]), ([15], [3]), ([16], [16]), ([17], [17]),
+    ([33, 0, 1, 128], [5, 33, 1, 2]), ([300], [60]), ([129, 517], [31, 65])])
+def test_rows_of_trees(dtype, H, Hkv, hd, T, rows):
+    c = Case(dtype, H, Hkv, hd, T, rows)
+    print("[attend]", dtype, H, Hkv, hd, T, rows, flush=True)
+    c.check(c.run())
+
+
+@pytest.mark.parametrize("dtype,H,Hkv,hd", SHAPES[:1] + SHAPES[-1:])
+@pytest.mark.parametrize("T,rows", [([4097], [1]), ([9000, 3, 5000], [1, 1, 2]),
+                                    ([2500], [130])])
+def test_long_prefixes_take_splits(dtype, H, Hkv, hd, T, rows):
+    c = Case(dtype, H, Hkv, hd, T, rows, seed=1)
+    sample = sorted({0, 1, c.n_rows // 2, c.n_rows - 1})
+    print("[attend]", dtype, T, rows, flush=True)
+    c.check(c.run(), rows=sample)
+    # the page table's capacity as the bound: another plan, the same answer
+    c.check(c.run(max_prefix=0), rows=sample)
+
+
+@pytest.mark.parametrize("dtype,H,Hkv,hd", [SHAPES[0], SHAPES[4]])
+@pytest.mark.parametrize("window,sinks", [(1, 0), (1, 1), (7, 4), (16, 0), (40, 17),
+                                          (100, 3), (2 ** 31 - 1, 2 ** 31 - 1),
+                                          (5, 1000)])
+@pytest.mark.parametrize("T,rows", [([200, 3, 0], [33, 4, 1]), ([2000], [1])])
+def test_window_and_sinks(dtype, H, Hkv, hd, window, sinks, T, rows):
+    c = Case(dtype, H, Hkv, hd, T, rows, seed=2, window=window, sinks=sinks)
+    print("[window]", dtype, window, sinks, T, flush=True)
+    c.check(c.run())
+
+
+def test_window_of_rows_far_from_their_prefix():
+    """Positions past, before and far below the prefix: windows that end
+    before it, inside it, and that nothing of it lies in."""
+    c = Case("bf16", 8, 2, 128, [100], [6], seed=3, window=20, sinks=2)
+    c.pos[:] = [0, 50, 119, 120, 2 ** 31 - 1, -2 ** 31]
+    c.check(c.run())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_that_see_nothing_are_zero(dtype):
+    c = Case(dtype, 8, 2, 128, [40, 0, 7], [4, 3, 2], seed=4, window=1, sinks=0)
+    c.pos[:] = 1000                 # the window lies past every prefix
+    c.vis[:] = 0
+    c.vis[1, 0] = 2                 # but for one row's own slot
+    got = c.run(fill=7.0)
+    c.check(got)
+    assert (got[[0, 2, 3, 4, 5, 6, 7, 8]] == 0).all() and (got[1] != 0).any()
+
+
+@pytest.mark.parametrize("dtype,hd", [("bf16", 128), ("bf16", 64), ("f32", 64)])
+def test_no_segment(dtype, hd):
+    c = Case(dtype, 8, 2, hd, [50, 0], [3, 2], seed=5, seg=False)
+    got = c.run(fill=3.0)
+    c.check(got)
+    assert (got[3:] == 0).all()
+
+
+@pytest.mark.parametrize("dtype,hd", [("bf16", 128), ("bf16", 64), ("f32", 64),
+                                      ("f32", 128)])
+def test_hidden_entries_add_nothing_whatever_they_hold(dtype, hd):
+    """NaN codes past the prefix, between the sinks and the window, and NaN
+    and infinities in segment slots that a row does not see."""
+    c = Case(dtype, 4, 2, hd, [70, 33], [20, 5], seed=6, window=24, sinks=3)
+    clean = c.run()
+    # past the prefix, and pages of the table past it
+    for s in range(2):
+        p, t = c.T[s] // 16, c.T[s] % 16
+        for codes, is_v in ((c.k, False), (c.v, True)):
+            for h in range(c.Hkv):
+                pg = c.table[s, p]
+                x = (ref.v_from_page(codes[0, pg, h], hd) if is_v
+                     else codes[0, pg, h].reshape(16, hd)).copy()
+                x[t:] = 0x7F
+                codes[0, pg, h] = ref.v_to_page(x) if is_v else x.reshape(-1)
+            codes[0, c.table[s, p + 1:]] = 0xFF
+    # entry 20 of sequence 0: hidden from every row (window 24 at 70 and on)
+    for codes, is_v in ((c.k, False), (c.v, True)):
+        for h in range(c.Hkv):
+            pg = c.table[0, 1]
+            x = (ref.v_from_page(codes[0, pg, h], hd) if is_v
+                 else codes[0, pg, h].reshape(16, hd)).copy()
+            x[4] = 0x7F
+            codes[0, pg, h] = ref.v_to_page(x) if is_v else x.reshape(-1)
+    for s, n in enumerate(c.rows):      # unused slots of the last segment page
+        sl = n % 16
+        if sl:
+            c.sk_t[s, n // 16, :, sl:] = float("nan")
+            c.sv_t[s, n // 16, :, :, sl:] = float("inf")
+    assert np.array_equal(c.run(), clean)
+    # values that some rows see and others do not
+    for slot, bad in ((3, float("inf")), (4, float("nan")), (5, float("-inf"))):
+        c.sv_t[0, 0, :, 7, slot] = bad
+    got = c.run()
+    for i in range(c.off[1]):
+        sees = [(int(c.vis[i, 0]) >> j) & 1 for j in (3, 4, 5)]
+        want = clean[i].copy()
+        if any(sees):
+            want[:, 7] = (np.nan if sees[1] or (sees[0] and sees[2])
+                          else np.inf if sees[0] else -np.inf)
+        assert np.array_equal(got[i], want, equal_nan=True), i
+    assert np.array_equal(got[c.off[1]:], clean[c.off[1]:])
+
+
+def test_nan_codes_inside_some_windows():
+    """A NaN V value of the prefix reaches the rows whose window it is in."""
+    c = Case("bf16", 4, 2, 128, [64], [12], seed=7, window=8, sinks=0)
+    clean = c.run()
+    x = ref.v_from_page(c.v[0, c.table[0, 3], 1], 128).copy()
+    x[11, 5] = 0x7F                     # entry 59
+    c.v[0, c.table[0, 3], 1] = ref.v_to_page(x)
+    got = c.run()
+    for i in range(12):
+        want = clean[i].copy()
+        if 59 > c.pos[i] - 8:
+            want[2:, 5] = np.nan        # KV head 1: query heads 2 and 3
+        assert np.array_equal(got[i], want, equal_nan=True), i
+
+
+def test_large_scores_and_a_late_maximum():
+    """Scores of hundreds that rise along the prefix, and all below zero."""
+    c = Case("bf16", 4, 1, 64, [600], [2], seed=8)
+    c.ke[:] = np.clip(118 + np.arange(c.ke.shape[1]) % 14, 1, 254)[None, :, None]
+    c.check(c.run())
+    c.k[:] = 0x38                       # every key 1.0
+    c.q_t[:] = -30.0
+    c.check(c.run())
+
+
+def test_rows_and_lengths_are_cut_to_the_buffers():
+    """Offsets, lengths and counts past what the caller's buffers hold; rows
+    behind the last sequence and past rows_per_seq stay as they were."""
+    c = Case("bf16", 8, 2, 128, [40, 20], [4, 3], seed=9)
+    base = c.run()
+    off = c.off.copy()
+    c.off = np.array([0, 4, 1000], np.int32)
+    c.T = [40, 20]
+    assert np.array_equal(c.run(rows_per_seq=4), base)
+    c.off = np.array([-5, 4, 7], np.int32)
+    assert np.array_equal(c.run(rows_per_seq=4), base)
+    c.off = np.array([0, 4, 6], np.int32)
+    got = c.run(fill=5.0)
+    assert np.array_equal(got[:6], base[:6]) and (got[6] == 5).all()
+    c.off = off
+    got = c.run(fill=5.0, rows_per_seq=3)
+    assert np.array_equal(got[[0, 1, 2, 4, 5, 6]], base[[0, 1, 2, 4, 5, 6]])
+    assert (got[3] == 5).all()
+    # a prefix length past the page table is cut to it
+    c2 = Case("f32", 4, 4, 64, [48], [1], seed=10, max_pages=3)
+    base = c2.run()
+    c2.T = [2 ** 31 - 1]
+    assert np.array_equal(c2.run(max_prefix=0), base)
+    c2.T = [-7]
+    got = c2.run(max_prefix=0)
+    c2.T = [0]
+    assert np.array_equal(got, c2.run(max_prefix=0))
+
+
+def test_out_of_range_pages_are_clamped():
+    c = Case("bf16", 8, 2, 128, [40], [2], seed=11)
+    n = c.k.shape[1]
+    t = c.table.copy()
+    c.table[0, :2] = [0, n - 1]
+    want = c.run()
+    c.table = t
+    c.table[0, :2] = [-3, n + 12345]
+    assert np.array_equal(c.run(), want)
+
+
+def test_layers_and_offsets_past_32_bits():
+    """The second layer of a pool of 2^32 codes and more."""
+    hkv, hd = 8, 128
+    n_pages = (1 << 32) // (hkv * 16 * hd) + 40
+    shape = kc().Shape(8, hkv, hd, "bf16", 1, 4)
+    dev = "cuda"
+    k = torch.zeros(2, n_pages, hkv, 16 * hd, dtype=torch.uint8, device=dev)
+    v = torch.zeros_like(k)
+    e = torch.full((2, n_pages, hkv), 127, dtype=torch.uint8, device=dev)
+    pages = torch.tensor([[n_pages - 1, 3, n_pages - 2, 0]], dtype=torch.int32)
+    c = Case("bf16", 8, hkv, hd, [50], [1], seed=12, max_pages=4, spare=0)
+    for j in range(4):
+        k[1, pages[0, j]] = torch.from_numpy(c.k[0, c.table[0, j]]).cuda()
+        v[1, pages[0, j]] = torch.from_numpy(c.v[0, c.table[0, j]]).cuda()
+    c.ke[:], c.ve[:] = 127, 127
+    cache = kc().QuantKV(shape, k, v, e, e.clone(), pages.to(dev))
+    d = lambda a: torch.from_numpy(np.ascontiguousarray(a)).cuda()  # noqa: E731
+    plan = kc().Attention(cache, d(c.off), None, d(np.array([50], np.int32)),
+                          d(c.seg_len), d(c.vis.view(np.int32)), c.sk_t.cuda(),
+                          c.sv_t.cuda(), n_rows=1, rows_per_seq=1)
+    got = plan(1, c.q_t.cuda()).float().cpu().numpy()
+    c.check(got)
+
+
+def test_runs_repeat_on_streams_and_in_graphs():
+    """Bit-identical runs, a second stream, a captured graph replayed between
+    eager calls of another plan."""
+    c = Case("bf16", 8, 2, 128, [3000, 900], [20, 64], seed=13)
+    first = c.run()
+    assert np.array_equal(c.run(), first)
+    plan, q = c.plan(), c.q_t.cuda()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        o = plan(0, q)
+    torch.cuda.current_stream().wait_stream(side)
+    assert np.array_equal(o.float().cpu().numpy(), first)
+    out = torch.zeros_like(q)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        plan(0, q, out)
+    other = c.plan()
+    for _ in range(3):
+        out.zero_()
+        other(0, q)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert np.array_equal(out.float().cpu().numpy(), first)
