@@ -16,6 +16,7 @@ import numpy as np
 import torch
 
 from . import binding as B
+from . import kvcache
 
 
 def _ptr(t):
@@ -44,11 +45,16 @@ class Runtime:
     tensors; ``None`` generates N(0, 0.02) weights on the device.
     prefill_rows: prompt rows that a prefill pass may take (the workspace is
     sized for them; prefill_chunk is the least).
+    kvq: the target's committed K/V in 8 bits, pages of both models from one
+    pool (``self.kvq``, ``self.pool``): prefill fills the element-type cache
+    and stores it, verify, commit and fork use the 8-bit one.  window, sinks:
+    what the verification sees of a long prefix (0, 0: all of it).
     """
 
     def __init__(self, w, weights=None, *, n_seqs=None, max_pages=None,
                  prefill_chunk=128, device="cuda", page_seed=3, seed=0,
-                 adapt_cap=0, share_layers=False, prefill_rows=2048):
+                 adapt_cap=0, share_layers=False, prefill_rows=2048, kvq=False,
+                 window=0, sinks=0):
         self.lib = B.load()
         self.w = w
         self.dev = torch.device(device)
@@ -91,7 +97,11 @@ class Runtime:
         B.check(self.lib, ctx, self.lib.sb_bind(
             ctx, C.byref(self.tw_c), C.byref(self.dw_c),
             _ptr(self.workspace), nbytes))
+        self.window, self.sinks = window, sinks
+        self.kvq = self.pool = None
         self._buffers(page_seed)
+        if kvq:
+            self._quantised()
 
     # ------------------------------------------------------------------
     def _weights(self, src, seed):
@@ -256,6 +266,21 @@ class Runtime:
                                      "r_reject")])
         self.V = V
 
+    def _quantised(self):
+        """The 8-bit target cache, and one page table and pool for it, the
+        drafter's cache and the element-type cache that prefill fills."""
+        s, w = self.w.target, self.w
+        shape = kvcache.Shape(s.n_heads, s.n_kv_heads, s.head_dim, w.dtype,
+                              self.S, self.max_pages)
+        n_pages = self.tk.shape[1]
+        self.pool = kvcache.PagePool.empty(shape, n_pages, self.tk.device)
+        self.tpt = self.dpt = self.pool.page_table
+        self.staging = kvcache.PagedKV(shape, self.tk, self.tv, self.tpt)
+        self.draft_kv = kvcache.PagedKV(shape, self.dk, self.dv, self.dpt)
+        self.tkv_c, self.dkv_c = self.staging.c, self.draft_kv.c
+        self.kvq = kvcache.QuantKV.empty(shape, s.n_layers, n_pages, self.tpt)
+        self.pool.attach([self.draft_kv, self.kvq])
+
     # ------------------------------------------------------------------
     @property
     def stream(self):
@@ -272,9 +297,15 @@ class Runtime:
             arr[i, :len(p)] = p
         self.prompt_dev = torch.from_numpy(arr).to(self.dev)
         clens = (C.c_int32 * self.S)(*lens)
+        if self.kvq is not None:
+            dlens = torch.tensor(lens, dtype=torch.int32).to(self.dev)
+            self.pool.reset()
+            self.pool.grow(dlens)
         self._check(self.lib.sb_prefill(
             self.ctx, C.byref(self.seqs_c), _ptr(self.prompt_dev), ld, clens,
             C.byref(self.tkv_c), C.byref(self.dkv_c), self.stream))
+        if self.kvq is not None:
+            self.kvq.store(self.staging, torch.zeros_like(dlens), dlens, ld)
 
     def expand(self, m, want_logits=False):
         if want_logits:
@@ -299,6 +330,12 @@ class Runtime:
         lg = self.vout["logits"] if want_logits else None
         self.vout_c = B.VerifyOut(_ptr(self.vout["argmax"]),
                                   _ptr(self.vout["taps"]), _ptr(lg))
+        if self.kvq is not None:
+            self._check(self.lib.sb_tree_verify_kvq(
+                self.ctx, C.byref(self.seqs_c), C.byref(self.tree_c),
+                C.byref(self.kvq.c), self.window, self.sinks,
+                C.byref(self.vout_c), self.stream))
+            return
         self._check(self.lib.sb_tree_verify(
             self.ctx, C.byref(self.seqs_c), C.byref(self.tree_c),
             C.byref(self.tkv_c), C.byref(self.vout_c), self.stream))
@@ -334,6 +371,14 @@ class Runtime:
     def commit(self):
         vc = B.VerifyOut(_ptr(self.vout["argmax"]), _ptr(self.vout["taps"]),
                          C.c_void_p(0))
+        if self.kvq is not None:
+            # pages for what this commit may add
+            self.pool.grow(self.T, self.w.M * self.w.K + 1)
+            self._check(self.lib.sb_commit_kvq(
+                self.ctx, C.byref(self.seqs_c), C.byref(self.tree_c),
+                C.byref(vc), C.byref(self.aout_c), C.byref(self.kvq.c),
+                C.byref(self.dkv_c), self.stream))
+            return
         self._check(self.lib.sb_commit(
             self.ctx, C.byref(self.seqs_c), C.byref(self.tree_c),
             C.byref(vc), C.byref(self.aout_c), C.byref(self.tkv_c),
@@ -345,6 +390,15 @@ class Runtime:
         self.verify()
         self.accept()
         self.commit()
+
+    def fork(self, parents, children):
+        """Sequences children[i] become continuations of parents[i] from their
+        present state (kvq only): full pages shared, the last one copied."""
+        self.pool.fork(parents, children, self.T)
+        a = torch.tensor(list(parents), device=self.dev)
+        b = torch.tensor(list(children), device=self.dev)
+        for t in (self.root, self.T, self.cond_taps):
+            t[b] = t[a]
 
     def set_length_bound(self, max_T: int):
         """Bound of T over all sequences (0: unknown); needed after writing
