@@ -597,7 +597,7 @@ int sb_kvq_store(const sb_cache_shape* shape, int32_t n_seqs, const sb_kv* src,
 typedef struct sb_attn_rows {
   int32_t n_seqs;              /* host, 1..max_seqs                          */
   int32_t n_rows;              /* host: rows of q, out, pos and vis          */
-  int32_t rows_per_seq;        /* host: most rows of one sequence, 1..65535;
+  int32_t rows_per_seq;        /* host: most rows of one sequence, 1..16384;
                                   rows of a sequence past it are not computed */
   int32_t max_prefix;          /* host bound of prefix_len; 0: the page
                                   table's capacity.  Entries past it are not

@@ -74,8 +74,8 @@ int check_rows(const sb_cache_shape* s, const sb_attn_rows* r, int window,
     return fail2(SB_ESHAPE, call, "n_seqs must be in 1..max_seqs");
   if (r->n_rows < 1 || r->n_rows > (1 << 22))
     return fail2(SB_ESHAPE, call, "n_rows must be in 1..2^22");
-  if (r->rows_per_seq < 1 || r->rows_per_seq > 65535)
-    return fail2(SB_ESHAPE, call, "rows_per_seq must be in 1..65535");
+  if (r->rows_per_seq < 1 || r->rows_per_seq > 16384)
+    return fail2(SB_ESHAPE, call, "rows_per_seq must be in 1..16384");
   if (r->max_prefix < 0) return fail2(SB_EINVAL, call, "max_prefix is negative");
   if (r->vis_words < 0 || r->vis_words > 16)
     return fail2(SB_ESHAPE, call, "vis_words must be in 0..16");
@@ -134,28 +134,25 @@ int check_pool(const sb_cache_shape* s, const sb_pool* p, const char* call) {
 int regions(const sb_cache_shape* s, const sb_pool* p, const sb_kv* kv,
             const sb_kvq* kvq, PoolRegions* out, const char* call) {
   out->n = 0;
-  auto add = [&](void* base, long long bytes, int layers) {
-    out->r[out->n++] = PoolRegion{static_cast<char*>(base), bytes, layers};
-  };
-  const long long elems = (long long)s->n_kv_heads * 16 * s->head_dim;
+  const int elems = s->n_kv_heads * 16 * s->head_dim;
   if (kv) {
     const int rc = check_elem_kv(kv, call);
     if (rc) return rc;
     if (kv->n_pages != p->n_pages || kv->page_table != p->page_table)
       return fail2(SB_EINVAL, call, "the cache has another page table or page count");
-    const long long b = elems * (s->dtype == SB_BF16 ? 2 : 4);
-    add(kv->k, b, kv->n_layers);
-    add(kv->v, b, kv->n_layers);
+    out->r[out->n++] = PoolRegion{static_cast<char*>(kv->k), static_cast<char*>(kv->v),
+                                  nullptr, nullptr,
+                                  elems * (s->dtype == SB_BF16 ? 2 : 4), 0,
+                                  kv->n_layers};
   }
   if (kvq) {
     const int rc = check_kvq(kvq, call);
     if (rc) return rc;
     if (kvq->n_pages != p->n_pages || kvq->page_table != p->page_table)
       return fail2(SB_EINVAL, call, "the 8-bit cache has another page table or page count");
-    add(kvq->k, elems, kvq->n_layers);
-    add(kvq->v, elems, kvq->n_layers);
-    add(kvq->k_exp, s->n_kv_heads, kvq->n_layers);
-    add(kvq->v_exp, s->n_kv_heads, kvq->n_layers);
+    out->r[out->n++] = PoolRegion{reinterpret_cast<char*>(kvq->k),
+                                  reinterpret_cast<char*>(kvq->v), kvq->k_exp,
+                                  kvq->v_exp, elems, s->n_kv_heads, kvq->n_layers};
   }
   return SB_OK;
 }

@@ -46,6 +46,7 @@ struct QRows {
 struct QPlan {
   int n_split;
   int split_tokens;
+  int qt;                    // tiles of 16 query vectors per workgroup
 };
 QPlan kvq_attn_plan(int n_seqs, int rows_per_seq, int max_prefix, int window,
                     int sinks, int H, int Hkv, int hd, int es, int max_split);
@@ -78,14 +79,18 @@ struct PoolList {            // sequences of a call, by value
   unsigned char a[64];
   unsigned char b[64];
 };
-struct PoolRegion {          // memory of one cache: [n_layers][n_pages][bytes]
-  char* base;
-  long long page_bytes;
+struct PoolRegion {          // one cache: k, v [n_layers][n_pages][page_bytes]
+  char* k;
+  char* v;
+  uint8_t* k_exp;            // [n_layers][n_pages][exp_bytes], if any
+  uint8_t* v_exp;
+  int page_bytes;            // of 16 tokens of K or V, a multiple of 16
+  int exp_bytes;
   int n_layers;
 };
 struct PoolRegions {
   int n;
-  PoolRegion r[6];
+  PoolRegion r[2];
 };
 void launch_pool_reset(const sb_pool& p, int max_seqs, int max_pages,
                        hipStream_t st);

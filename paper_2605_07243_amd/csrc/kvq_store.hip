@@ -23,6 +23,73 @@
 namespace sb {
 namespace {
 
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+typedef short s16x2 __attribute__((ext_vector_type(2)));
+
+// Four values as they are stored.  top: the largest bits of |x|, non-finite
+// ones included (bf16: of even and odd values, as halves); code: e4m3 of
+// x / scale, ties to even, what is not finite as NaN (v_cvt_scalef32_pk_fp8:
+// two values an instruction; checked exact for every bf16 value and the scale
+// range in use).
+template <typename T> struct Quad;
+template <> struct Quad<bf16_t> {
+  u32x2 w;
+  __device__ __forceinline__ void set(int e, bf16_t v) {
+    w[e >> 1] |= (uint32_t)v << (16 * (e & 1));
+  }
+  __device__ __forceinline__ void keep(uint32_t use) {
+    w[0] &= (use & 1u ? 0xFFFFu : 0u) | (use & 2u ? 0xFFFF0000u : 0u);
+    w[1] &= (use & 4u ? 0xFFFFu : 0u) | (use & 8u ? 0xFFFF0000u : 0u);
+  }
+  __device__ __forceinline__ static uint32_t join(uint32_t a, uint32_t b) {
+    return __builtin_bit_cast(uint32_t,
+                              __builtin_elementwise_max(__builtin_bit_cast(u16x2, a),
+                                                        __builtin_bit_cast(u16x2, b)));
+  }
+  __device__ __forceinline__ uint32_t top(uint32_t t) const {
+    return join(t, join(w[0] & 0x7FFF7FFFu, w[1] & 0x7FFF7FFFu));
+  }
+  __device__ __forceinline__ static uint32_t bits(uint32_t t) {
+    return max(t & 0xFFFFu, t >> 16) << 16;
+  }
+  __device__ __forceinline__ float at(int e) const {
+    return __uint_as_float(e & 1 ? w[e >> 1] & 0xFFFF0000u : w[e >> 1] << 16);
+  }
+  __device__ __forceinline__ uint32_t code(float scale) const {
+    const uint32_t lo = w[0], hi = w[1];   // (an element cannot be bit-cast itself)
+    s16x2 r = {0, 0};
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, __builtin_bit_cast(bf16x2_t, lo),
+                                                  scale, false);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, __builtin_bit_cast(bf16x2_t, hi),
+                                                  scale, true);
+    return __builtin_bit_cast(uint32_t, r);
+  }
+};
+template <> struct Quad<float> {
+  u32x4 w;
+  __device__ __forceinline__ void set(int e, float v) { w[e] = __float_as_uint(v); }
+  __device__ __forceinline__ void keep(uint32_t use) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (!((use >> e) & 1u)) w[e] = 0u;
+  }
+  __device__ __forceinline__ uint32_t top(uint32_t t) const {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) t = max(t, w[e] & 0x7FFFFFFFu);
+    return t;
+  }
+  __device__ __forceinline__ static uint32_t bits(uint32_t t) { return t; }
+  __device__ __forceinline__ float at(int e) const { return __uint_as_float(w[e]); }
+  __device__ __forceinline__ uint32_t code(float scale) const {
+    s16x2 r = {0, 0};
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, at(0), at(1), scale, false);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, at(2), at(3), scale, true);
+    return __builtin_bit_cast(uint32_t, r);
+  }
+};
+
 // Entries of a paged elem cache.
 template <typename T>
 struct CacheSource {
@@ -51,35 +118,28 @@ struct CacheSource {
     const size_t off = (((size_t)l * n_pages + pg) * Hkv + kh) * 16 * hd;
     return Page{k + off, v + off};
   }
-  // eight K values of slot t, four V values of slots t .. t + 3
+  // eight K values of slot t; four V values of slots t .. t + 3 (zeros where
+  // none is used)
   __device__ __forceinline__ void k8(const Page& p, int t, int c, int hd,
-                                     bool, float (&x)[8]) const {
-    Frag8<T> f;
-    f.load(p.k + t * hd + c);
-    if constexpr (sizeof(T) == 2) {
-      const uint32_t w[4] = {f.v.x, f.v.y, f.v.z, f.v.w};
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        x[2 * e] = __uint_as_float(w[e] << 16);
-        x[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
+                                     bool use, Quad<T> (&x)[2]) const {
+    x[0] = x[1] = Quad<T>{};
+    if (use) {
+      const Quad<T>* q = reinterpret_cast<const Quad<T>*>(p.k + t * hd + c);
+      if constexpr (sizeof(T) == 2) {   // (one 16-byte load)
+        const u32x4 w = *reinterpret_cast<const u32x4*>(q);
+        x[0].w = w.xy;
+        x[1].w = w.zw;
+      } else {
+        x[0] = q[0];
+        x[1] = q[1];
       }
-    } else {
-      x[0] = f.a.x; x[1] = f.a.y; x[2] = f.a.z; x[3] = f.a.w;
-      x[4] = f.b.x; x[5] = f.b.y; x[6] = f.b.z; x[7] = f.b.w;
     }
   }
-  __device__ __forceinline__ void v4(const Page& p, int t, int c, int,
-                                     uint32_t, float (&x)[4]) const {
-    if constexpr (sizeof(T) == 2) {
-      const uint2 w = *reinterpret_cast<const uint2*>(p.v + c * 16 + t);
-      x[0] = __uint_as_float(w.x << 16);
-      x[1] = __uint_as_float(w.x & 0xFFFF0000u);
-      x[2] = __uint_as_float(w.y << 16);
-      x[3] = __uint_as_float(w.y & 0xFFFF0000u);
-    } else {
-      const float4 w = *reinterpret_cast<const float4*>(p.v + c * 16 + t);
-      x[0] = w.x; x[1] = w.y; x[2] = w.z; x[3] = w.w;
-    }
+  __device__ __forceinline__ Quad<T> v4(const Page& p, int t, int c,
+                                        uint32_t use) const {
+    Quad<T> x{};
+    if (use) x = *reinterpret_cast<const Quad<T>*>(p.v + c * 16 + t);
+    return x;
   }
 };
 
@@ -120,51 +180,41 @@ struct PathSource {
     return min(max(j <= 0 ? 0 : p.path[j - 1], 0), seg_pages * 16 - 1);
   }
   __device__ __forceinline__ void k8(const Page& p, int t, int c, int hd,
-                                     bool use, float (&x)[8]) const {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = 0.f;
+                                     bool use, Quad<T> (&x)[2]) const {
+    x[0] = x[1] = Quad<T>{};
     if (!use) return;
     const int sl = slot(p, t);
-    const T* r = p.k + (sl >> 4) * p.step + (sl & 15) * hd + c;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = Elem<T>::to_f32(r[e]);
+    const Quad<T>* q = reinterpret_cast<const Quad<T>*>(
+        p.k + (sl >> 4) * p.step + (sl & 15) * hd + c);
+    x[0] = q[0];
+    x[1] = q[1];
   }
-  __device__ __forceinline__ void v4(const Page& p, int t, int c, int,
-                                     uint32_t use, float (&x)[4]) const {
+  __device__ __forceinline__ Quad<T> v4(const Page& p, int t, int c,
+                                        uint32_t use) const {
+    Quad<T> x{};
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      x[e] = 0.f;
       if (!((use >> e) & 1u)) continue;
       const int sl = slot(p, t + e);
-      x[e] = Elem<T>::to_f32(p.v[(sl >> 4) * p.step + c * 16 + (sl & 15)]);
+      x.set(e, p.v[(sl >> 4) * p.step + c * 16 + (sl & 15)]);
     }
+    return x;
   }
 };
 
-// |x| for the largest value: infinities and NaN do not set the scale
-__device__ __forceinline__ float finite_abs(float x) {
-  const float a = fabsf(x);
-  return a < __builtin_inff() ? a : 0.f;
-}
-// the least e >= -126 with amax <= 448 * 2^e
-__device__ __forceinline__ int exponent_for(float amax) {
-  const uint32_t u = __float_as_uint(amax);
+// the least e >= -126 with amax <= 448 * 2^e (bits of amax >= 0, finite)
+__device__ __forceinline__ int exponent_for(uint32_t u) {
   const int E = (int)(u >> 23) - 127;
   return max(E - ((u & 0x7FFFFFu) <= 0x600000u ? 8 : 7), -126);
 }
-// four values to codes; what is not finite becomes NaN
-__device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d) {
-  auto clean = [](float x) {
-    return fabsf(x) < __builtin_inff() ? x : __builtin_nanf("");
-  };
-  int w = __builtin_amdgcn_cvt_pk_fp8_f32(clean(a), clean(b), 0, false);
-  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(clean(c), clean(d), w, true);
-}
-// held codes times 2^d (d <= 0), rounded again
-__device__ __forceinline__ uint32_t lower4(uint32_t w, float f) {
+// held codes over 2^n (scale = 2^n, n >= 0), rounded again
+__device__ __forceinline__ uint32_t lower4(uint32_t w, float scale) {
   const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(w, false);
   const auto hi = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
-  return codes4(lo[0] * f, lo[1] * f, hi[0] * f, hi[1] * f);
+  s16x2 r = {0, 0};
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, lo[0], lo[1], scale, false);
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, hi[0], hi[1], scale, true);
+  return __builtin_bit_cast(uint32_t, r);
 }
 __device__ __forceinline__ uint32_t byte_mask(uint32_t bits4) {
   return (bits4 & 1u ? 0xFFu : 0u) | (bits4 & 2u ? 0xFF00u : 0u) |
@@ -177,7 +227,7 @@ __global__ __launch_bounds__(256) void kvq_store_kernel(Source src, sb_kvq dst,
                                                         int* err) {
   const int s = blockIdx.y, l = blockIdx.z;
   const int lane = threadIdx.x & 63;
-  const int task = blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int task = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const bool is_v = task & 1;
   const int kh = (task >> 1) % Hkv, jp = (task >> 1) / Hkv;
   int a, z;
@@ -196,78 +246,91 @@ __global__ __launch_bounds__(256) void kvq_store_kernel(Source src, sb_kvq dst,
   uint8_t* expo = (is_v ? dst.v_exp : dst.k_exp) + block;
   const auto page = src.page(l, s, j, kh, Hkv, HD, 0);
   constexpr int NW = HD / 16;      // words of four codes a lane owns
-  float x[NW][4];
-  float amax = 0.f;
+  Quad<T> x[NW];
   const int va = lane >> 4, vr = lane & 15;
+  // V: which of the lane's four slots are stored, and which are held; what is
+  // there already is loaded with the new values (one round trip)
+  const uint32_t use = (fresh >> (4 * va)) & 15u;
+  const uint32_t kept = (((1u << t0) - 1u) >> (4 * va)) & 15u;
+  const int own = t0 > 0 ? min((int)*expo - 127, 127) : -126;
+  u32x4 was[NW / 4];
+#pragma unroll
+  for (int c = 0; c < NW / 4; ++c) was[c] = u32x4{0, 0, 0, 0};
   if (is_v) {
-    const uint32_t use = (fresh >> (4 * va)) & 15u;
+    if (use != 15u && (use | kept) != 0) {
 #pragma unroll
-    for (int c = 0; c < NW; ++c) src.v4(page, 4 * va, 16 * c + vr, HD, use, x[c]);
+      for (int c = 0; c < NW / 4; ++c)
+        was[c] = reinterpret_cast<const u32x4*>(code)[lane * (NW / 4) + c];
+    }
 #pragma unroll
-    for (int c = 0; c < NW; ++c)
+    for (int c = 0; c < NW; ++c) x[c] = src.v4(page, 4 * va, 16 * c + vr, use);
+    if (use != 15u) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if ((use >> e) & 1u) amax = fmaxf(amax, finite_abs(x[c][e]));
+      for (int c = 0; c < NW; ++c) x[c].keep(use);
+    }
   } else {
 #pragma unroll
     for (int i = 0; i < NW / 2; ++i) {
       const int e0 = (i * 64 + lane) * 8, t = e0 / HD;
-      float y[8];
+      Quad<T> y[2];
       src.k8(page, t, e0 % HD, HD, (fresh >> t) & 1u, y);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        x[2 * i + (e >> 2)][e & 3] = y[e];
-        if ((fresh >> t) & 1u) amax = fmaxf(amax, finite_abs(y[e]));
-      }
+      x[2 * i] = y[0];
+      x[2 * i + 1] = y[1];
     }
   }
-  amax = wave_max(amax);
-  int e = exponent_for(amax), drop = 0;
-  if (t0 > 0) {
-    const int was = min((int)*expo - 127, 127);
-    drop = max(was - e, 0);          // the page's own is the larger one
-    e += drop;
-    drop = was - e;                  // <= 0: held codes go down by this
-  }
-  const float f = __uint_as_float((uint32_t)(127 - e) << 23);
-  const float g = __uint_as_float((uint32_t)(127 + max(drop, -60)) << 23);
-  const bool whole = fresh == 0xFFFFu;
-  if (is_v) {
-    uint32_t w[NW];
-    uint32_t* o = reinterpret_cast<uint32_t*>(code) + lane * NW;
-    const uint32_t mf = byte_mask((fresh >> (4 * va)) & 15u);
-    const uint32_t mh = byte_mask((((1u << t0) - 1u) >> (4 * va)) & 15u);
+  uint32_t top = 0;
+#pragma unroll
+  for (int c = 0; c < NW; ++c) top = x[c].top(top);
+  // (bits of non-negative floats are ordered as integers)
+  top = (uint32_t)-wave_min_i(-(int)Quad<T>::bits(top));
+  if (top >= 0x7F800000u) {            // what is not finite sets no scale
+    uint32_t m = 0;
 #pragma unroll
     for (int c = 0; c < NW; ++c)
-      w[c] = codes4(x[c][0] * f, x[c][1] * f, x[c][2] * f, x[c][3] * f);
-    if (!whole) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t u = __float_as_uint(x[c].at(e)) & 0x7FFFFFFFu;
+        m = max(m, u < 0x7F800000u ? u : 0u);
+      }
+    top = (uint32_t)-wave_min_i(-(int)m);
+  }
+  const int e = max(exponent_for(top), own);
+  const bool rise = t0 > 0 && e > own;
+  const float scale = __uint_as_float((uint32_t)(127 + e) << 23);
+  const float down = __uint_as_float((uint32_t)(127 + min(e - own, 60)) << 23);
+  if (lane == 0) *expo = (uint8_t)(e + 127);
+  if (is_v) {
+    // groups of four slots without a new value whose codes stay are not touched
+    if (use == 0 && (kept == 0 || !rise)) return;
+    uint32_t w[NW];
+#pragma unroll
+    for (int c = 0; c < NW; ++c) w[c] = x[c].code(scale);
+    if (use != 15u) {
+      const uint32_t mf = byte_mask(use), mh = byte_mask(kept);
 #pragma unroll
       for (int c = 0; c < NW; ++c) {
-        const uint32_t old = o[c];
-        const uint32_t h = drop < 0 ? lower4(old, g) : old;
+        const uint32_t old = was[c / 4][c % 4];
+        const uint32_t h = rise ? lower4(old, down) : old;
         w[c] = (w[c] & mf) | (h & mh) | (old & ~(mf | mh));
       }
     }
 #pragma unroll
-    for (int c = 0; c < NW; c += 4)
-      *reinterpret_cast<uint4*>(o + c) = make_uint4(w[c], w[c + 1], w[c + 2], w[c + 3]);
+    for (int c = 0; c < NW / 4; ++c)
+      reinterpret_cast<u32x4*>(code)[lane * (NW / 4) + c] =
+          u32x4{w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]};
   } else {
 #pragma unroll
     for (int i = 0; i < NW / 2; ++i) {
       const int e0 = (i * 64 + lane) * 8, t = e0 / HD;
-      uint2* o = reinterpret_cast<uint2*>(code + e0);
+      u32x2* o = reinterpret_cast<u32x2*>(code + e0);
       if ((fresh >> t) & 1u) {
-        const float(&p)[4] = x[2 * i];
-        const float(&q)[4] = x[2 * i + 1];
-        *o = make_uint2(codes4(p[0] * f, p[1] * f, p[2] * f, p[3] * f),
-                        codes4(q[0] * f, q[1] * f, q[2] * f, q[3] * f));
-      } else if (t < t0 && drop < 0) {
-        const uint2 old = *o;
-        *o = make_uint2(lower4(old.x, g), lower4(old.y, g));
+        *o = u32x2{x[2 * i].code(scale), x[2 * i + 1].code(scale)};
+      } else if (t < t0 && rise) {
+        const u32x2 old = *o;
+        *o = u32x2{lower4(old[0], down), lower4(old[1], down)};
       }
     }
   }
-  if (lane == 0) *expo = (uint8_t)(e + 127);
 }
 
 template <typename T, typename Source>

@@ -8,7 +8,7 @@
 // counts are added to with atomics, and sums of ones have no order.
 //
 // The bookkeeping is a few launches of a few microseconds; copies run at the
-// rate of a plain copy (16 KiB or 32 KiB runs of 16-byte accesses).
+// rate of a plain copy.
 #include <algorithm>
 
 #include "bounds.h"
@@ -18,6 +18,8 @@
 
 namespace sb {
 namespace {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kChunk = 8192;          // pages that one workgroup walks at a time
 // scratch: number of moves; live pages per chunk; sources; targets; new number
@@ -33,7 +35,8 @@ __host__ __device__ inline size_t map_at(int n) { return kLists + 2 * ((size_t)n
 template <typename Pred, typename Fn>
 __device__ __forceinline__ int walk_chunk(int base, int n_pages, int before,
                                           int* cnt, Pred pred, Fn fn) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   unsigned long long mask[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
@@ -45,15 +48,16 @@ __device__ __forceinline__ int walk_chunk(int base, int n_pages, int before,
 #pragma unroll
     for (int j = 0; j < 8; ++j) cnt[j * 16 + wave] = __popcll(mask[j]);
   __syncthreads();
-  int mine[8], total = 0;
+  // every wave scans the 128 counts, two a lane (each at most 64)
+  const int2 c = reinterpret_cast<const int2*>(cnt)[lane];
+  int total;
+  const int excl = wave_excl_scan_small<8>(c.x + c.y, total);
+  int mine[8];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) mine[j] = 0;
-  for (int i = 0; i < 128; ++i) {
-    const int c = cnt[i];
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (i == j * 16 + wave) mine[j] = total;
-    total += c;
+  for (int j = 0; j < 8; ++j) {
+    const int i = (j * 16 + wave) >> 1;
+    mine[j] = __builtin_amdgcn_readlane(excl, i) +
+              (wave & 1 ? __builtin_amdgcn_readlane(c.x, i) : 0);
   }
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
@@ -104,7 +108,7 @@ __device__ __forceinline__ int request_of(const int* off, int n, int rank) {
 __global__ __launch_bounds__(1024) void pool_grow_kernel(sb_pool p, int n_seqs,
                                                          const int* __restrict__ len,
                                                          int extra, int max_pages) {
-  __shared__ int cnt[128], off[65], have[64], over[64];
+  __shared__ __attribute__((aligned(8))) int cnt[128], off[65], have[64], over[64];
   const int t = threadIdx.x;
   if (t < 64) {
     int need = 0;
@@ -158,7 +162,7 @@ __global__ __launch_bounds__(1024) void pool_release_kernel(sb_pool p, PoolList 
 __global__ __launch_bounds__(1024) void pool_fork_kernel(sb_pool p, PoolList l,
                                                          const int* __restrict__ len,
                                                          int max_pages) {
-  __shared__ int cnt[128], off[65], full[64];
+  __shared__ __attribute__((aligned(8))) int cnt[128], off[65], full[64];
   const int t = threadIdx.x;
   auto length = [&](int i) {
     const int s = l.a[i];
@@ -209,8 +213,10 @@ __global__ __launch_bounds__(1024) void pool_fork_kernel(sb_pool p, PoolList l,
   }
 }
 
-// Copies the listed pages in every region and layer.  moved: their counts and
-// new numbers are set, too.
+// Copies the listed pages in every layer of the caches, a (page, layer) of K
+// and V at a time: 32 KiB in an 8-bit cache of 8 x 128 heads, eight 16-byte
+// loads a thread before the first store.  moved: the counts and new numbers of
+// the pages are set, too.
 __global__ __launch_bounds__(256) void pool_copy_kernel(sb_pool p, PoolRegions rg,
                                                         int units, int moved) {
   const int n = p.scratch[0];
@@ -219,36 +225,50 @@ __global__ __launch_bounds__(256) void pool_copy_kernel(sb_pool p, PoolRegions r
   const long long total = (long long)n * units;
   for (long long u = blockIdx.x; u < total; u += gridDim.x) {
     const int i = (int)(u / units);
-    int k = (int)(u % units);
+    int k = (int)(u - (long long)i * units);
     const int a = src[i], b = dst[i];
     if (moved && k == 0 && threadIdx.x == 0) {
       p.scratch[map_at(p.n_pages) + a] = b;
       p.refs[b] = p.refs[a];
       p.refs[a] = 0;
     }
-    for (int r = 0; r < rg.n; ++r) {
-      const PoolRegion& g = rg.r[r];
-      if (k >= g.n_layers) {
-        k -= g.n_layers;
-        continue;
+    if (rg.n == 0) continue;
+    const bool second = k >= rg.r[0].n_layers;
+    if (second) k -= rg.r[0].n_layers;
+    const PoolRegion g = second ? rg.r[1] : rg.r[0];
+    const size_t layer = (size_t)k * p.n_pages;
+    const int m = (int)(g.page_bytes >> 4);
+    const u32x4* ks = reinterpret_cast<const u32x4*>(g.k) + (layer + a) * m;
+    const u32x4* vs = reinterpret_cast<const u32x4*>(g.v) + (layer + a) * m;
+    u32x4* kd = reinterpret_cast<u32x4*>(g.k) + (layer + b) * m;
+    u32x4* vd = reinterpret_cast<u32x4*>(g.v) + (layer + b) * m;
+    for (int e = threadIdx.x; e < m; e += 1024) {
+      u32x4 x[4], y[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int c = min(e + 256 * j, m - 1);
+        x[j] = ks[c];
+        y[j] = vs[c];
       }
-      char* base = g.base + (size_t)k * p.n_pages * g.page_bytes;
-      const char* from = base + (size_t)a * g.page_bytes;
-      char* to = base + (size_t)b * g.page_bytes;
-      if ((g.page_bytes & 15) == 0 && ((uintptr_t)g.base & 15) == 0) {
-        const int m = (int)(g.page_bytes >> 4);
-        for (int e = threadIdx.x; e < m; e += 256)
-          reinterpret_cast<uint4*>(to)[e] = reinterpret_cast<const uint4*>(from)[e];
-      } else {
-        for (int e = threadIdx.x; e < g.page_bytes; e += 256) to[e] = from[e];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int c = e + 256 * j;
+        if (c < m) {
+          kd[c] = x[j];
+          vd[c] = y[j];
+        }
       }
-      break;
+    }
+    if (g.exp_bytes > 0 && (int)threadIdx.x < 2 * g.exp_bytes) {
+      const int h = (int)threadIdx.x % g.exp_bytes;
+      uint8_t* x = (int)threadIdx.x < g.exp_bytes ? g.k_exp : g.v_exp;
+      x[(layer + b) * g.exp_bytes + h] = x[(layer + a) * g.exp_bytes + h];
     }
   }
 }
 
 __global__ __launch_bounds__(1024) void pool_count_kernel(sb_pool p) {
-  __shared__ int cnt[128];
+  __shared__ __attribute__((aligned(8))) int cnt[128];
   const int n = walk_chunk(
       blockIdx.x * kChunk, p.n_pages, 0, cnt, [&](int pg) { return p.refs[pg] > 0; },
       [](int, int) {});
@@ -257,7 +277,7 @@ __global__ __launch_bounds__(1024) void pool_count_kernel(sb_pool p) {
 
 // Lists the pages in use at or above their number n, and the free ones below.
 __global__ __launch_bounds__(1024) void pool_moves_kernel(sb_pool p) {
-  __shared__ int cnt[128], red[3];
+  __shared__ __attribute__((aligned(8))) int cnt[128], red[3];
   const int t = threadIdx.x, nb = gridDim.x, base = blockIdx.x * kChunk;
   if (t < 3) red[t] = 0;
   __syncthreads();
@@ -271,8 +291,13 @@ __global__ __launch_bounds__(1024) void pool_moves_kernel(sb_pool p) {
   // in use below page n
   const int bb = n / kChunk;
   if (t < min(bb, nb)) atomicAdd(&red[2], p.scratch[kCounts + t]);
-  for (int pg = bb * kChunk + t; pg < min(n, p.n_pages); pg += 1024)
-    if (p.refs[pg] > 0) atomicAdd(&red[2], 1);
+  int some = 0;
+#pragma unroll
+  for (int j = 0; j < kChunk / 1024; ++j) {
+    const int pg = bb * kChunk + j * 1024 + t;
+    some += __popcll(__ballot(pg < min(n, p.n_pages) && p.refs[pg] > 0));
+  }
+  if ((t & 63) == 0) atomicAdd(&red[2], some);
   __syncthreads();
   const int low = red[2];
   int* src = p.scratch + src_at();

@@ -25,13 +25,19 @@ def _tensor(t, name, dtype, shape, device=None):
     return C.c_void_p(t.data_ptr())
 
 
+# handle of the current stream of a device (the integer alone: building a
+# torch.cuda.Stream for it costs as much as the rest of a call)
+_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda i: torch.cuda.current_stream(i).cuda_stream)
+
+
 def _call(device, fn, *args):
     """fn(*args, stream) with the tensors' device current; raises SBError."""
     if torch.cuda.current_device() == device.index:
-        rc = fn(*args, C.c_void_p(torch.cuda.current_stream(device).cuda_stream))
+        rc = fn(*args, _stream(device.index))
     else:
         with torch.cuda.device(device):
-            rc = fn(*args, C.c_void_p(torch.cuda.current_stream(device).cuda_stream))
+            rc = fn(*args, _stream(device.index))
     if rc != B.SB_OK:
         B.check(B.load(), None, rc)
 
@@ -143,18 +149,25 @@ class Attention:
             raise B.SBError(B.SB_ESHAPE, self.lib.sb_last_error(None).decode())
         self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
         self._ws = C.c_void_p(self.workspace.data_ptr())
-        self._rows_shape = (n_rows, sh.n_heads, sh.head_dim)
+        self._rows_shape = torch.Size((n_rows, sh.n_heads, sh.head_dim))
+        self._nbytes = nbytes
+        self._attend = self.lib.sb_kvq_attend
+
+    def _fits(self, t):
+        return (t.dtype is self.cache.shape.elem and t.shape == self._rows_shape
+                and t.device == self.device and t.is_contiguous())
 
     def __call__(self, layer, q, out=None):
         """Attention outputs of the rows, [n_rows][n_heads][head_dim]."""
         if out is None:
             out = torch.empty_like(q)
-        el = self.cache.shape.elem
-        a = _tensor(q, "q", el, self._rows_shape, self.device)
-        o = _tensor(out, "out", el, self._rows_shape, self.device)
-        _call(self.device, self.lib.sb_kvq_attend, self.cache.shape.c, self.cache.c,
-              layer, self.rows, a, self.window, self.sinks, o, self._ws,
-              self.workspace.numel())
+        if not (self._fits(q) and self._fits(out)):
+            raise ValueError(
+                f"q and out must be contiguous {self.cache.shape.elem} tensors of "
+                f"shape {tuple(self._rows_shape)} on {self.device}")
+        _call(self.device, self._attend, self.cache.shape.c, self.cache.c, layer,
+              self.rows, q.data_ptr(), self.window, self.sinks, out.data_ptr(),
+              self._ws, self._nbytes)
         return out
 
 

@@ -108,7 +108,7 @@ def test_store(lib):  # noqa: F811
 @pytest.mark.parametrize("kw,code", [
     (dict(n_seqs=0), B.SB_ESHAPE), (dict(n_seqs=5), B.SB_ESHAPE),
     (dict(n_rows=0), B.SB_ESHAPE), (dict(n_rows=(1 << 22) + 1), B.SB_ESHAPE),
-    (dict(rows_per_seq=0), B.SB_ESHAPE), (dict(rows_per_seq=65536), B.SB_ESHAPE),
+    (dict(rows_per_seq=0), B.SB_ESHAPE), (dict(rows_per_seq=16385), B.SB_ESHAPE),
     (dict(max_prefix=-1), B.SB_EINVAL), (dict(vis_words=17), B.SB_ESHAPE),
     (dict(vis_words=-1), B.SB_ESHAPE), (dict(seg_pages=33), B.SB_ESHAPE),
     (dict(seg_pages=-1), B.SB_ESHAPE)])
