@@ -814,7 +814,7 @@ void layer_body(sb_ctx* c, const sb_layer_weights& lw, int layer,
                    pf.window, pf.sinks};
     const QPlan plan =
         kvq_attn_plan(p.n_seqs, rows_per_seq, max_prefix, pf.window, pf.sinks,
-                      D.H, D.Hkv, D.hd, D.es, D.n_split);
+                      D.H, D.Hkv, D.es, D.n_split);
     ProfScope ps(c, st, SB_PROF_ATTN);
     launch_kvq_attn<T>(static_cast<const T*>(c->q), qr, qv, D.H, D.Hkv, D.hd,
                        plan, c->o_part, c->ml, A, st);

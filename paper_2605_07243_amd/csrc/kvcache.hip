@@ -96,8 +96,7 @@ int most_rows(const sb_attn_rows* r) { return std::min(r->rows_per_seq, r->n_row
 
 QPlan plan_of(const sb_cache_shape* s, const sb_attn_rows* r, int window, int sinks) {
   return kvq_attn_plan(r->n_seqs, most_rows(r), prefix_bound(s, r), window, sinks,
-                       s->n_heads, s->n_kv_heads, s->head_dim,
-                       s->dtype == SB_BF16 ? 2 : 4, 64);
+                       s->n_heads, s->n_kv_heads, s->dtype == SB_BF16 ? 2 : 4, 64);
 }
 
 size_t align_up(size_t x) { return (x + 255) / 256 * 256; }

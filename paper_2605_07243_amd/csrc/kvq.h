@@ -46,10 +46,10 @@ struct QRows {
 struct QPlan {
   int n_split;
   int split_tokens;
-  int qt;                    // tiles of 16 query vectors per workgroup
+  int width;                 // query vectors per workgroup: 16 or 32
 };
 QPlan kvq_attn_plan(int n_seqs, int rows_per_seq, int max_prefix, int window,
-                    int sinks, int H, int Hkv, int hd, int es, int max_split);
+                    int sinks, int H, int Hkv, int es, int max_split);
 // o_part [n_split][n_rows][H][hd], ml [n_split][n_rows][H][2] (fp32; unused
 // with one split).
 template <typename T>

@@ -38,8 +38,7 @@ namespace {
 // finite, so that exp2(score - reference) of a hidden key (-inf) is 0
 constexpr float kLow = -3.0e38f;
 constexpr float kLog2e = 1.4426950408889634f;
-// waves of a workgroup; each takes every kWaves-th tile of 32 keys
-constexpr int kWaves = 4;
+constexpr int NW = 4;         // waves of a workgroup
 constexpr int kMaxSplit = 64;
 
 __device__ __forceinline__ float byte_scale(int b) {
@@ -88,6 +87,14 @@ __device__ __forceinline__ void unpack8(const Frag8<bf16_t>& f, float (&v)[8]) {
 __device__ __forceinline__ void unpack8(const Frag8<float>& f, float (&v)[8]) {
   v[0] = f.a.x; v[1] = f.a.y; v[2] = f.a.z; v[3] = f.a.w;
   v[4] = f.b.x; v[5] = f.b.y; v[6] = f.b.z; v[7] = f.b.w;
+}
+
+__device__ __forceinline__ void store4(bf16_t* p, float4 v) {
+  *reinterpret_cast<uint2*>(p) =
+      make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
+}
+__device__ __forceinline__ void store4(float* p, float4 v) {
+  *reinterpret_cast<float4*>(p) = v;
 }
 
 // What a hidden key may not do to the rows that do not see it: its probability
@@ -194,36 +201,46 @@ __device__ __forceinline__ void rows_of(const QRows& r, int s, int& row0, int& n
 }
 __device__ __forceinline__ int wave_max_i(int v) { return -wave_min_i(-v); }
 
-// A workgroup: QT tiles of 16 query vectors of one KV head, one split of the
-// prefix; the last split also takes the segment.  Each of the four waves holds
-// all of the workgroup's queries and takes every fourth tile of 32 keys (no
-// barrier in the loop), one tile of loads ahead; their (O, m, l) meet in LDS at
-// the end.  A tile's codes are converted once for the QT query tiles.
-template <typename T, int HD, int QT>
-__global__ __launch_bounds__(kWaves * 64, 2) void kvq_attn_kernel(
-    const T* __restrict__ q, QRows r, QView kv, int H, int Hkv, int n_split,
-    int split_tokens, float scale, float* __restrict__ o_part,
+// What a workgroup works on.  The dispatcher deals workgroups out round-robin
+// over the 8 XCDs; (sequence, KV head, split) items go round with it, so that
+// ragged sequences spread over the chip, and the query groups of an item, which
+// read the same pages, follow each other on one XCD.
+struct Item {
+  int qg, s, kh, z;
+};
+__device__ __forceinline__ Item item_of(int groups, int n_seqs, int Hkv) {
+  const unsigned b = blockIdx.x, y = b >> 3;
+  Item i;
+  i.qg = (int)(y % (unsigned)groups);
+  const unsigned n = y / (unsigned)groups * 8 + (b & 7);
+  i.kh = (int)(n % (unsigned)Hkv);
+  const unsigned t = n / (unsigned)Hkv;
+  i.s = (int)(t % (unsigned)n_seqs);
+  i.z = (int)(t / (unsigned)n_seqs);
+  return i;
+}
+
+// A workgroup: 16 query vectors of one KV head, one split of the prefix; the
+// last split also takes the segment.  Each of its NW waves holds all of the
+// queries and takes every NW-th tile of 32 keys (no barrier in the loop), one
+// tile of loads ahead; their (O, m, l) meet in LDS at the end.
+template <typename T, int HD>
+__global__ __launch_bounds__(NW * 64, 2) void kvq_attn_kernel(
+    const T* __restrict__ q, QRows r, QView kv, int groups, int H, int Hkv,
+    int n_split, int split_tokens, float scale, float* __restrict__ o_part,
     float* __restrict__ ml, T* __restrict__ out) {
   constexpr int NK = HD / 32;          // contraction steps of a score
   constexpr int NC = HD / 16;          // output column blocks
   constexpr int W4 = HD / 64;          // 16-byte loads per page half
   constexpr int LDO = HD + 4;
-  __shared__ __attribute__((aligned(16))) float osh[kWaves][16][LDO];
-  __shared__ float msh[QT][kWaves][16], lsh[QT][kWaves][16];
-  int bx = blockIdx.x, by = blockIdx.y, bz = blockIdx.z;
-  {
-    // the query groups of a split on one XCD: they read the same pages
-    const int gx = gridDim.x, gz = gridDim.z;
-    const int l = xcd_grouped(bx + gx * (by + (int)gridDim.y * bz),
-                              gx * (int)gridDim.y * gz);
-    bx = l % gx;
-    bz = (l / gx) % gz;
-    by = l / (gx * gz);
-  }
-  const int s = by / Hkv, kh = by % Hkv, G = H / Hkv;
+  __shared__ __attribute__((aligned(16))) float osh[NW][16][LDO];
+  __shared__ float msh[NW][16], lsh[NW][16];
+  const Item it = item_of(groups, r.n_seqs, Hkv);
+  const int s = it.s, kh = it.kh, bz = it.z, G = H / Hkv;
+  if (bz >= n_split) return;
   int row0, n_rows;
   rows_of(r, s, row0, n_rows);
-  const int nq = n_rows * G, q0 = bx * 16 * QT;
+  const int nq = n_rows * G, q0 = it.qg * 16;
   if (q0 >= nq) return;
   const int Tp = prefix_of(r, kv, s);
   const int ns = splits_of(r, Tp, n_split, split_tokens);
@@ -231,40 +248,27 @@ __global__ __launch_bounds__(kWaves * 64, 2) void kvq_attn_kernel(
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c16 = lane & 15, g = lane >> 4;
-  int row[QT], lo[QT];
-  Frag8<T> qf[QT][NK];
-#pragma unroll
-  for (int j = 0; j < QT; ++j) {
-    const int qv = q0 + 16 * j + c16;
+  Frag8<T> qf[NK];
+  int row, lo = 0;                     // lo: first entry of the row's window
+  {
+    const int qv = q0 + c16;
     const bool valid = qv < nq;
     const int rq = valid ? div_small(qv, G) : 0;
-    row[j] = row0 + rq;
+    row = row0 + rq;
     const int head = kh * G + (valid ? qv - rq * G : 0);
 #pragma unroll
     for (int i = 0; i < NK; ++i) {
-      qf[j][i].load(q + ((size_t)row[j] * H + head) * HD + g * (HD / 4) + 8 * i);
-      if (!valid) qf[j][i].zero();
+      qf[i].load(q + ((size_t)row * H + head) * HD + g * (HD / 4) + 8 * i);
+      if (!valid) qf[i].zero();
     }
-    // first entry of the row's window
-    lo[j] = 0;
-    if (r.window > 0)
-      lo[j] = (int)max(0LL, min((long long)r.pos[row[j]] - (r.window - 1), (long long)Tp));
   }
   int lo_min = 0, lo_max = 0;
   if (r.window > 0) {
-    lo_min = lo_max = lo[0];
-#pragma unroll
-    for (int j = 1; j < QT; ++j) {
-      lo_min = min(lo_min, lo[j]);
-      lo_max = max(lo_max, lo[j]);
-    }
-    lo_min = __builtin_amdgcn_readfirstlane(wave_min_i(lo_min));
-    lo_max = __builtin_amdgcn_readfirstlane(wave_max_i(lo_max));
-    if (lo_max <= r.sinks) {     // the sinks reach into every window
-      lo_min = lo_max = 0;
-#pragma unroll
-      for (int j = 0; j < QT; ++j) lo[j] = 0;
-    }
+    lo = (int)max(0LL, min((long long)r.pos[row] - (r.window - 1), (long long)Tp));
+    lo_min = __builtin_amdgcn_readfirstlane(wave_min_i(lo));
+    lo_max = __builtin_amdgcn_readfirstlane(wave_max_i(lo));
+    // (the sinks reach into every window)
+    if (lo_max <= r.sinks) lo = lo_min = lo_max = 0;
   }
   const Span sp = make_span(Tp, r.sinks, lo_min, lo_max);
   const int* ptab = kv.page_table + (size_t)s * kv.max_pages;
@@ -274,54 +278,40 @@ __global__ __launch_bounds__(kWaves * 64, 2) void kvq_attn_kernel(
   const int f0 = min(max(sp.full0, t0), t1), f1 = max(f0, min(sp.full1, t1));
   scale *= kLog2e;
 
-  float m[QT], l[QT];
-  f32x4_t acc[QT][NC];
+  float m = kLow, l = 0.f;
+  f32x4_t acc[NC];
 #pragma unroll
-  for (int j = 0; j < QT; ++j) {
-    m[j] = kLow;
-    l[j] = 0.f;
-#pragma unroll
-    for (int c = 0; c < NC; ++c) acc[j][c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  }
+  for (int c = 0; c < NC; ++c) acc[c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
   // softmax step: raw scores of the two halves times k0, k1 (> 0) ->
   // probabilities, packed
-  auto soften = [&](f32x4_t (&sc)[QT][2], float k0, float k1, Frag8<T> (&pf)[QT]) {
+  auto soften = [&](f32x4_t (&sc)[2], float k0, float k1, Frag8<T>& pf) {
     // (compared with the raw scores: a maximum of matrix results costs two
     // instructions each; the border need not be exact)
-    const float r0 = __builtin_amdgcn_rcpf(k0), r1 = __builtin_amdgcn_rcpf(k1);
+    const float b0 = (m + 8.f) * __builtin_amdgcn_rcpf(k0);
+    const float b1 = (m + 8.f) * __builtin_amdgcn_rcpf(k1);
     bool up = false;
 #pragma unroll
-    for (int j = 0; j < QT; ++j) {
-      const float b0 = (m[j] + 8.f) * r0, b1 = (m[j] + 8.f) * r1;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) up |= (sc[j][0][e] > b0) | (sc[j][1][e] > b1);
-    }
+    for (int e = 0; e < 4; ++e) up |= (sc[0][e] > b0) | (sc[1][e] > b1);
     if (__ballot(up) != 0) {
+      const float mx = fmaxf(
+          k0 * fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3])),
+          k1 * fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
+      const float m2 = fmaxf(m, max_x32(max_x16(mx)));
+      const float a = __builtin_amdgcn_exp2f(m - m2);
+      m = m2;
+      l *= a;
 #pragma unroll
-      for (int j = 0; j < QT; ++j) {
-        const float mx = fmaxf(
-            k0 * fmaxf(fmaxf(sc[j][0][0], sc[j][0][1]), fmaxf(sc[j][0][2], sc[j][0][3])),
-            k1 * fmaxf(fmaxf(sc[j][1][0], sc[j][1][1]), fmaxf(sc[j][1][2], sc[j][1][3])));
-        const float m2 = fmaxf(m[j], max_x32(max_x16(mx)));
-        const float a = __builtin_amdgcn_exp2f(m[j] - m2);
-        m[j] = m2;
-        l[j] *= a;
-#pragma unroll
-        for (int c = 0; c < NC; ++c) acc[j][c] *= a;
-      }
+      for (int c = 0; c < NC; ++c) acc[c] *= a;
     }
+    float p[8];
 #pragma unroll
-    for (int j = 0; j < QT; ++j) {
-      float p[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        p[e] = __builtin_amdgcn_exp2f(
-            __builtin_fmaf(sc[j][e >> 2][e & 3], e < 4 ? k0 : k1, -m[j]));
-        l[j] += p[e];
-      }
-      pack8(pf[j], p);
+    for (int e = 0; e < 8; ++e) {
+      p[e] = __builtin_amdgcn_exp2f(
+          __builtin_fmaf(sc[e >> 2][e & 3], e < 4 ? k0 : k1, -m));
+      l += p[e];
     }
+    pack8(pf, p);
   };
 
   const size_t page_bytes = (size_t)Hkv * 16 * HD;
@@ -340,9 +330,9 @@ __global__ __launch_bounds__(kWaves * 64, 2) void kvq_attn_kernel(
   // whole tiles, 32 of this wave's at a time: lane 2 n + h holds page h of
   // tile n
   uint4 kr[2][2][W4], vr[2][2][W4];
-  for (int n0 = 0; f0 + wave + kWaves * n0 < f1; n0 += 32) {
-    const int cnt = min(32, (f1 - f0 - wave + kWaves - 1) / kWaves - n0);
-    const int v_l = min(2 * (f0 + wave + kWaves * (n0 + (lane >> 1))) + (lane & 1),
+  for (int n0 = 0; f0 + wave + NW * n0 < f1; n0 += 32) {
+    const int cnt = min(32, (f1 - f0 - wave + NW - 1) / NW - n0);
+    const int v_l = min(2 * (f0 + wave + NW * (n0 + (lane >> 1))) + (lane & 1),
                         sp.n - 1);
     const int pid = checked_index(ptab[sp.page(v_l)], kv.n_pages, kv.err, kDevPage);
     const int ke_l = kv.k_exp[(size_t)pid * Hkv + kh];
@@ -353,21 +343,19 @@ __global__ __launch_bounds__(kWaves * 64, 2) void kvq_attn_kernel(
         load_page(__builtin_amdgcn_readlane(pid, 2 * n + h), kd[h], vd[h]);
     };
     auto compute = [&](int n, const uint4 (&kd)[2][W4], const uint4 (&vd)[2][W4]) {
-      f32x4_t sc[QT][2];
+      f32x4_t sc[2];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-#pragma unroll
-        for (int j = 0; j < QT; ++j) sc[j][h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+sc[h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
         const uint32_t* w = reinterpret_cast<const uint32_t*>(&kd[h][0]);
 #pragma unroll
         for (int i = 0; i < NK; ++i) {
           Frag8<T> kf;
           cvt8(kf, w[2 * i], 1.f, w[2 * i + 1], 1.f);
-#pragma unroll
-          for (int j = 0; j < QT; ++j) sc[j][h] = mma_16x16x32(kf, qf[j][i], sc[j][h]);
+          sc[h] = mma_16x16x32(kf, qf[i], sc[h]);
         }
       }
-      Frag8<T> pf[QT];
+      Frag8<T> pf;
       soften(sc, byte_scale(__builtin_amdgcn_readlane(ke_l, 2 * n)) * scale,
              byte_scale(__builtin_amdgcn_readlane(ke_l, 2 * n + 1)) * scale, pf);
       const float vs0 = byte_scale(__builtin_amdgcn_readlane(ve_l, 2 * n));
@@ -378,8 +366,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void kvq_attn_kernel(
       for (int c = 0; c < NC; ++c) {
         Frag8<T> vf;
         cvt8(vf, w0[c], vs0, w1[c], vs1);
-#pragma unroll
-        for (int j = 0; j < QT; ++j) acc[j][c] = mma_16x16x32(vf, pf[j], acc[j][c]);
+        acc[c] = mma_16x16x32(vf, pf, acc[c]);
       }
     };
     issue(0, kr[0], vr[0]);
@@ -399,16 +386,12 @@ __global__ __launch_bounds__(kWaves * 64, 2) void kvq_attn_kernel(
   if (bz == ns - 1 && kv.seg_pages > 0 && r.vis_words > 0)
     L = max(0, min(min(r.seg_len[s], kv.seg_pages * 16), r.vis_words * 32));
   const int n_gen = n_pre + ((L + 31) >> 5);
-  for (int i = (wave + kWaves - (f1 - f0) % kWaves) % kWaves; i < n_gen; i += kWaves) {
+  for (int i = (wave + NW - (f1 - f0) % NW) % NW; i < n_gen; i += NW) {
     Frag8<T> vf[NC];
-    f32x4_t sc[QT][2];
+    f32x4_t sc[2];
     float ks[2];
-    uint32_t seen[QT];
-#pragma unroll
-    for (int j = 0; j < QT; ++j) {
-      seen[j] = 0;
-      sc[j][0] = sc[j][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    }
+    uint32_t seen = 0;                 // bit e: key of score e
+    sc[0] = sc[1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     if (i < n_pre) {
       const int v0 = 2 * (i < n_left ? t0 + i : f1 + i - n_left);
       int first[2];                    // entry number of each half
@@ -430,8 +413,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void kvq_attn_kernel(
         for (int c = 0; c < NK; ++c) {
           Frag8<T> kf;
           cvt8(kf, w[2 * c], 1.f, w[2 * c + 1], 1.f);
-#pragma unroll
-          for (int j = 0; j < QT; ++j) sc[j][h] = mma_16x16x32(kf, qf[j][c], sc[j][h]);
+          sc[h] = mma_16x16x32(kf, qf[c], sc[h]);
         }
       }
       const uint32_t* w0 = reinterpret_cast<const uint32_t*>(&vd[0][0]);
@@ -439,12 +421,10 @@ __global__ __launch_bounds__(kWaves * 64, 2) void kvq_attn_kernel(
 #pragma unroll
       for (int c = 0; c < NC; ++c) cvt8(vf[c], w0[c], vs[0], w1[c], vs[1]);
 #pragma unroll
-      for (int j = 0; j < QT; ++j)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int key = first[e >> 2] + 4 * g + (e & 3);
-          seen[j] |= (uint32_t)(key < Tp && (key < r.sinks || key >= lo[j])) << e;
-        }
+      for (int e = 0; e < 8; ++e) {
+        const int key = first[e >> 2] + 4 * g + (e & 3);
+        seen |= (uint32_t)(key < Tp && (key < r.sinks || key >= lo)) << e;
+      }
     } else {
       const int t = i - n_pre;
       const T* kp[2];
@@ -460,8 +440,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void kvq_attn_kernel(
         for (int c = 0; c < NK; ++c) {
           Frag8<T> kf;
           kf.load(kp[h] + 8 * c);
-#pragma unroll
-          for (int j = 0; j < QT; ++j) sc[j][h] = mma_16x16x32(kf, qf[j][c], sc[j][h]);
+          sc[h] = mma_16x16x32(kf, qf[c], sc[h]);
         }
       }
 #pragma unroll
@@ -475,24 +454,19 @@ __global__ __launch_bounds__(kWaves * 64, 2) void kvq_attn_kernel(
           vf[c].b = *reinterpret_cast<const float4*>(vp[1] + 256 * c);
         }
       }
+      const uint32_t word = r.vis[(size_t)row * r.vis_words + t];
 #pragma unroll
-      for (int j = 0; j < QT; ++j) {
-        const uint32_t word = r.vis[(size_t)row[j] * r.vis_words + t];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int slot = 16 * (e >> 2) + 4 * g + (e & 3);
-          seen[j] |= (uint32_t)(((word >> slot) & 1u) && 32 * t + slot < L) << e;
-        }
+      for (int e = 0; e < 8; ++e) {
+        const int slot = 16 * (e >> 2) + 4 * g + (e & 3);
+        seen |= (uint32_t)(((word >> slot) & 1u) && 32 * t + slot < L) << e;
       }
     }
 #pragma unroll
-    for (int j = 0; j < QT; ++j)
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          sc[j][h][e] = (seen[j] >> (4 * h + e)) & 1u ? sc[j][h][e] : -__builtin_inff();
-    Frag8<T> pf[QT];
+      for (int e = 0; e < 4; ++e)
+        sc[h][e] = (seen >> (4 * h + e)) & 1u ? sc[h][e] : -__builtin_inff();
+    Frag8<T> pf;
     soften(sc, ks[0], ks[1], pf);
     uint32_t bad = 0;
 #pragma unroll
@@ -500,79 +474,489 @@ __global__ __launch_bounds__(kWaves * 64, 2) void kvq_attn_kernel(
     if (__ballot(bad != 0) != 0) {
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
-        const BadParts<T> b = take_bad(vf[c]);
-#pragma unroll
-        for (int j = 0; j < QT; ++j) acc[j][c] = add_bad(b, seen[j], acc[j][c]);
+        acc[c] = add_bad(take_bad(vf[c]), seen, acc[c]);
         __builtin_amdgcn_sched_barrier(0);   // (one column block at a time)
       }
     }
 #pragma unroll
     for (int c = 0; c < NC; ++c)
-#pragma unroll
-      for (int j = 0; j < QT; ++j) acc[j][c] = mma_16x16x32(vf[c], pf[j], acc[j][c]);
+      acc[c] = mma_16x16x32(vf[c], pf, acc[c]);
   }
 
-  // the waves' shares, one query tile after the other
+  // the waves' shares
+  l = sum_x32(sum_x16(l));
+  if (g == 0) {
+    msh[wave][c16] = m;
+    lsh[wave][c16] = l;
+  }
 #pragma unroll
-  for (int j = 0; j < QT; ++j) {
-    l[j] = sum_x32(sum_x16(l[j]));
-    if (g == 0) {
-      msh[j][wave][c16] = m[j];
-      lsh[j][wave][c16] = l[j];
+  for (int c = 0; c < NC; ++c)
+    *reinterpret_cast<float4*>(&osh[wave][c16][16 * c + 4 * g]) =
+        make_float4(acc[c][0], acc[c][1], acc[c][2], acc[c][3]);
+  __syncthreads();
+  constexpr int TPQ = NW * 64 / 16;     // threads of one query vector
+  const int qj = tid / TPQ, part = tid % TPQ, qv = q0 + qj;
+  if (qv >= nq) return;
+  float M = kLow, Lsum = 0.f, wt[NW];
+#pragma unroll
+  for (int w = 0; w < NW; ++w) M = fmaxf(M, msh[w][qj]);
+#pragma unroll
+  for (int w = 0; w < NW; ++w) {
+    wt[w] = __builtin_amdgcn_exp2f(msh[w][qj] - M);
+    Lsum += wt[w] * lsh[w][qj];
+  }
+  const int rq = div_small(qv, G);
+  const float inv = Lsum == 0.f ? 0.f : 1.0f / Lsum;
+  const size_t at = (size_t)(row0 + rq) * H + kh * G + qv - rq * G;
+#pragma unroll
+  for (int col = part * 4; col < HD; col += 4 * TPQ) {
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const float4 x = *reinterpret_cast<const float4*>(&osh[w][qj][col]);
+      o.x += wt[w] * x.x;
+      o.y += wt[w] * x.y;
+      o.z += wt[w] * x.z;
+      o.w += wt[w] * x.w;
+    }
+    if (ns > 1)
+      *reinterpret_cast<float4*>(
+          o_part + ((size_t)bz * r.n_rows * H + at) * HD + col) = o;
+    else
+      store4(out + at * HD + col, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+  }
+  if (ns > 1 && part == 0)
+    *reinterpret_cast<float2*>(ml + ((size_t)bz * r.n_rows * H + at) * 2) =
+        make_float2(M, Lsum);
+}
+
+// ---- bf16: 32 query vectors a wave ------------------------------------------
+//
+// v_mfma_f32_32x32x16_bf16 with 32 keys (two pages) as rows and 32 query vectors
+// as columns.  Its 32 cycles leave room for seven vector instructions, which
+// the 16x16 form's 16 cycles do not (measured, cycles per SIMD: 8 of the large
+// product with 64 FMAs 338, 16 of the small one with 64 FMAs 400, products or
+// FMAs alone 274 to 330): conversions and softmax run beside the products.
+//
+// Lane (r = lane % 32, h = lane / 32) holds half h of key r's K row (hd / 2
+// consecutive bytes), and of S^T the scores of query r for keys 4 h .. 4 h + 3
+// and 8 + 4 h .. of each page, the B operand of O^T += V^T P^T.  A operand: the
+// codes of those keys for columns 32 b + r, i.e. groups a = h and 2 + h of the
+// V page; lanes r and r + 16 each load half of the 16 columns' run and swap the
+// words that the other needs (v_permlane16_swap).
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ f32x16_t mma_32x32x16(const Frag8<bf16_t>& a,
+                                                 const Frag8<bf16_t>& b,
+                                                 f32x16_t acc) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+      __builtin_bit_cast(bf16x8_t, a.v), __builtin_bit_cast(bf16x8_t, b.v), acc,
+      0, 0, 0);
+}
+__device__ __forceinline__ f32x16_t zero16() {
+  f32x16_t z;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) z[i] = 0.f;
+  return z;
+}
+__device__ __forceinline__ f32x16_t add_bad32(const BadParts<bf16_t>& b,
+                                              uint32_t seen8, f32x16_t acc) {
+  float one[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) one[e] = (seen8 >> e) & 1u ? 1.f : 0.f;
+  Frag8<bf16_t> fs;
+  pack8(fs, one);
+  const f32x16_t nu = mma_32x32x16(b.up, fs, zero16());
+  const f32x16_t nd = mma_32x32x16(b.dn, fs, zero16());
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    if (nu[i] > 0.f) acc[i] += __builtin_inff();
+    if (nd[i] > 0.f) acc[i] -= __builtin_inff();
+  }
+  return acc;
+}
+
+template <int HD>
+__global__ __launch_bounds__(NW * 64, 2) void kvq_attn32_kernel(
+    const bf16_t* __restrict__ q, QRows r, QView kv, int groups, int H, int Hkv,
+    int n_split, int split_tokens, float scale, float* __restrict__ o_part,
+    float* __restrict__ ml, bf16_t* __restrict__ out) {
+  constexpr int NK = HD / 16;          // contraction steps of a score
+  constexpr int NB = HD / 32;          // output column blocks
+  constexpr int LDO = HD + 4;
+  typedef Frag8<bf16_t> Frag;
+  typedef uint32_t vword __attribute__((ext_vector_type(HD / 32)));
+  __shared__ __attribute__((aligned(16))) float osh[NW][32][LDO];
+  __shared__ float msh[NW][32], lsh[NW][32];
+  const Item it = item_of(groups, r.n_seqs, Hkv);
+  const int s = it.s, kh = it.kh, bz = it.z, G = H / Hkv;
+  if (bz >= n_split) return;
+  int row0, n_rows;
+  rows_of(r, s, row0, n_rows);
+  const int nq = n_rows * G, q0 = it.qg * 32;
+  if (q0 >= nq) return;
+  const int Tp = prefix_of(r, kv, s);
+  const int ns = splits_of(r, Tp, n_split, split_tokens);
+  if (bz >= ns) return;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int c32 = lane & 31, h = lane >> 5;
+  Frag qf[NK];
+  int row, lo = 0;                     // lo: first entry of the row's window
+  {
+    const int qv = q0 + c32;
+    const bool valid = qv < nq;
+    const int rq = valid ? div_small(qv, G) : 0;
+    row = row0 + rq;
+    const int head = kh * G + (valid ? qv - rq * G : 0);
+    const bf16_t* qp = q + ((size_t)row * H + head) * HD + h * (HD / 2);
+#pragma unroll
+    for (int i = 0; i < NK; ++i) {
+      qf[i].load(qp + 8 * i);
+      if (!valid) qf[i].zero();
     }
   }
-  const int qj = tid >> 4, part16 = tid & 15;
-#pragma unroll
-  for (int j = 0; j < QT; ++j) {
-    if (q0 + 16 * j >= nq) break;      // uniform
-    if (j > 0) __syncthreads();
-#pragma unroll
-    for (int c = 0; c < NC; ++c)
-      *reinterpret_cast<float4*>(&osh[wave][c16][16 * c + 4 * g]) =
-          make_float4(acc[j][c][0], acc[j][c][1], acc[j][c][2], acc[j][c][3]);
-    __syncthreads();
-    const int qv = q0 + 16 * j + qj;
-    if (qv >= nq) continue;
-    float M = kLow, L = 0.f, wt[kWaves];
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) M = fmaxf(M, msh[j][w][qj]);
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      wt[w] = __builtin_amdgcn_exp2f(msh[j][w][qj] - M);
-      L += wt[w] * lsh[j][w][qj];
-    }
-    const int rq = div_small(qv, G);
-    const int orow = row0 + rq, ohead = kh * G + qv - rq * G;
-    const float inv = L == 0.f ? 0.f : 1.0f / L;
-    const size_t at = (size_t)orow * H + ohead;
-#pragma unroll
-    for (int e = 0; e < HD / 64; ++e) {
-      const int col = part16 * 4 + e * 64;
-      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
-        const float4 x = *reinterpret_cast<const float4*>(&osh[w][qj][col]);
-        o.x += wt[w] * x.x;
-        o.y += wt[w] * x.y;
-        o.z += wt[w] * x.z;
-        o.w += wt[w] * x.w;
-      }
-      if (ns > 1) {
-        *reinterpret_cast<float4*>(
-            o_part + ((size_t)bz * r.n_rows * H + at) * HD + col) = o;
-      } else if constexpr (sizeof(T) == 2) {
-        *reinterpret_cast<uint2*>(out + at * HD + col) =
-            make_uint2(pack_bf16x2(o.x * inv, o.y * inv),
-                       pack_bf16x2(o.z * inv, o.w * inv));
-      } else {
-        *reinterpret_cast<float4*>(out + at * HD + col) =
-            make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
-      }
-    }
-    if (ns > 1 && part16 == 0)
-      *reinterpret_cast<float2*>(ml + ((size_t)bz * r.n_rows * H + at) * 2) =
-          make_float2(M, L);
+  int lo_min = 0, lo_max = 0;
+  if (r.window > 0) {
+    lo = (int)max(0LL, min((long long)r.pos[row] - (r.window - 1), (long long)Tp));
+    lo_min = __builtin_amdgcn_readfirstlane(wave_min_i(lo));
+    lo_max = __builtin_amdgcn_readfirstlane(wave_max_i(lo));
+    // (the sinks reach into every window)
+    if (lo_max <= r.sinks) lo = lo_min = lo_max = 0;
   }
+  const Span sp = make_span(Tp, r.sinks, lo_min, lo_max);
+  const int* ptab = kv.page_table + (size_t)s * kv.max_pages;
+  const int tiles = (sp.n + 1) >> 1, per = (tiles + ns - 1) / ns;
+  const int t0 = bz * per, t1 = max(t0, min(tiles, t0 + per));
+  // this split's whole tiles, and what is left before and after them
+  const int f0 = min(max(sp.full0, t0), t1), f1 = max(f0, min(sp.full1, t1));
+  scale *= kLog2e;
+
+  float m = 0.f, l = 0.f, lim = -__builtin_inff();
+  f32x16_t acc[NB];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) acc[b] = zero16();
+
+  // raw scores of two pages -> score k - m, where the reference m moves when
+  // that exceeds `lim` somewhere (k0, k1 > 0: the pages' scales): 8, or anything
+  // a row sees while it has no reference yet
+  auto refer = [&](f32x16_t& sc, float k0, float k1) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sc[i] = __builtin_fmaf(sc[i], i < 8 ? k0 : k1, -m);
+    float top = fmaxf(sc[0], sc[1]);
+#pragma unroll
+    for (int i = 2; i < 16; i += 2) top = fmaxf(fmaxf(top, sc[i]), sc[i + 1]);
+    if (__ballot(top > lim) != 0) {
+      const float x = max_x32(top);
+      const bool move = x > lim, none = lim < 0.f;
+      const float d = move ? (none ? x : fmaxf(x, 0.f)) : 0.f;
+      const float a = none ? 1.f : __builtin_amdgcn_exp2f(-d);
+      lim = move ? 8.f : lim;
+      m += d;
+      l *= a;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sc[i] -= d;
+#pragma unroll
+      for (int b = 0; b < NB; ++b) acc[b] *= a;
+    }
+  };
+  // two probabilities, packed
+  auto weigh = [&](float x, float y) {
+    const float p = __builtin_amdgcn_exp2f(x), q = __builtin_amdgcn_exp2f(y);
+    l += p;
+    l += q;
+    return pack_bf16x2(p, q);
+  };
+  auto put = [](Frag (&pf)[2], int c, uint32_t w) {   // pair c of 8
+    Frag& f = pf[c / 4];
+    if (c % 4 == 0) f.v.x = w;
+    if (c % 4 == 1) f.v.y = w;
+    if (c % 4 == 2) f.v.z = w;
+    if (c % 4 == 3) f.v.w = w;
+  };
+
+  // a lane's codes: half a K row of the tile, and of each page of V half the
+  // words of groups h and 2 + h
+  typedef u32x4 KRaw[HD / 32];
+  typedef vword VRaw[2][2];
+  const size_t page_bytes = (size_t)Hkv * 16 * HD;
+  const uint8_t* kbase = kv.k + (size_t)kh * 16 * HD;
+  const uint8_t* vbase = kv.v + (size_t)kh * 16 * HD;
+  const uint32_t klane = (c32 & 15) * HD + h * (HD / 2);
+  const uint32_t vlane = (h * 16 + (c32 & 15)) * (HD / 4) + (c32 >> 4) * (HD / 8);
+  auto load_k = [&](int p0, int p1, KRaw& kq) {
+    const uint8_t* b0 = kbase + (size_t)p0 * page_bytes;
+    const uint8_t* b1 = kbase + (size_t)p1 * page_bytes;
+    const uint8_t* kp = (c32 < 16 ? b0 : b1) + klane;
+#pragma unroll
+    for (int j = 0; j < HD / 32; ++j)
+      kq[j] = *reinterpret_cast<const u32x4*>(kp + 16 * j);
+  };
+  auto load_v = [&](int p0, int p1, VRaw& vq) {
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      const uint8_t* vp = vbase + (size_t)(p ? p1 : p0) * page_bytes;
+#pragma unroll
+      for (int a = 0; a < 2; ++a)
+        vq[p][a] = *reinterpret_cast<const vword*>(vp + (vlane + a * 8 * HD));
+    }
+  };
+  auto k_frag = [&](const KRaw& kq, int i, Frag& f) {
+    cvt8(f, kq[i / 2][2 * (i % 2)], 1.f, kq[i / 2][2 * (i % 2) + 1], 1.f);
+  };
+  auto scores = [&](const KRaw& kq) {
+    f32x16_t sc = zero16();
+#pragma unroll
+    for (int i = 0; i < NK; ++i) {
+      Frag kf;
+      k_frag(kq, i, kf);
+      sc = mma_32x32x16(kf, qf[i], sc);
+    }
+    return sc;
+  };
+  // words of the V^T operands of page p: w[b][a], column block b, group h + 2 a
+  auto v_words = [&](const VRaw& vq, int p, uint32_t (&w)[NB][2]) {
+#pragma unroll
+    for (int a = 0; a < 2; ++a) {
+      vword v = vq[p][a];
+      // (taken apart here and not where a loop begins, which would wait for it)
+      __asm__ volatile("" : "+v"(v));
+#pragma unroll
+      for (int j = 0; j < NB / 2; ++j) {
+        const auto x = __builtin_amdgcn_permlane16_swap(v[2 * j], v[2 * j + 1],
+                                                        false, false);
+        w[j][a] = x[0];
+        w[NB / 2 + j][a] = x[1];
+      }
+    }
+  };
+
+  // whole tiles, 64 of this wave's at a time: lane n holds the pages and the
+  // four scale bytes of tile n.  The scores of tile n + 1 are formed beside the
+  // softmax of tile n; K of tile n + 3 and V of tile n + 2 are loaded into the
+  // registers that tile n leaves.
+  KRaw kq[2];
+  VRaw vq[2];
+  for (int n0 = 0; f0 + wave + NW * n0 < f1; n0 += 64) {
+    const int cnt = min(64, (f1 - f0 - wave + NW - 1) / NW - n0);
+    int id0, id1;
+    uint32_t ex;
+    {
+      const int v = 2 * (f0 + wave + NW * (n0 + min(lane, cnt - 1)));
+      id0 = checked_index(ptab[sp.page(v)], kv.n_pages, kv.err, kDevPage);
+      id1 = checked_index(ptab[sp.page(v + 1)], kv.n_pages, kv.err, kDevPage);
+      const size_t a0 = (size_t)id0 * Hkv + kh, a1 = (size_t)id1 * Hkv + kh;
+      ex = kv.k_exp[a0] | kv.k_exp[a1] << 8 | kv.v_exp[a0] << 16 | (uint32_t)kv.v_exp[a1] << 24;
+    }
+    // (past the last tile: the last one again)
+    auto fetch_k = [&](int n, KRaw& d) {
+      n = min(n, cnt - 1);
+      load_k(__builtin_amdgcn_readlane(id0, n), __builtin_amdgcn_readlane(id1, n), d);
+    };
+    auto fetch_v = [&](int n, VRaw& d) {
+      n = min(n, cnt - 1);
+      load_v(__builtin_amdgcn_readlane(id0, n), __builtin_amdgcn_readlane(id1, n), d);
+    };
+    fetch_k(0, kq[1]);
+    fetch_k(1, kq[0]);
+    fetch_v(0, vq[0]);
+    f32x16_t sc = scores(kq[1]);
+    fetch_k(2, kq[1]);
+    __builtin_amdgcn_sched_barrier(0);   // (loads in the order of the loop)
+    fetch_v(1, vq[1]);
+    // one tile: kn holds K of tile n + 1, vn V of tile n (the barriers keep the
+    // compiler from taking the vector instructions ahead of the products)
+    auto step = [&](int n, KRaw& kn, VRaw& vn) {
+      const uint32_t e = __builtin_amdgcn_readlane(ex, n);
+      refer(sc, byte_scale(e & 255) * scale, byte_scale((e >> 8) & 255) * scale);
+      f32x16_t next = zero16();
+      Frag pf[2], f;
+      k_frag(kn, 0, f);
+#pragma unroll
+      for (int i = 0; i < NK; ++i) {
+        next = mma_32x32x16(f, qf[i], next);
+        if (i + 1 < NK) k_frag(kn, i + 1, f);
+#pragma unroll
+        for (int c = i * (8 / NK); c < (i + 1) * (8 / NK); ++c)
+          put(pf, c, weigh(sc[2 * c], sc[2 * c + 1]));
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      fetch_k(n + 3, kn);
+      sc = next;
+      uint32_t w[2][NB][2];
+      v_words(vn, 0, w[0]);
+      const float v0 = byte_scale((e >> 16) & 255), v1 = byte_scale(e >> 24);
+      cvt8(f, w[0][0][0], v0, w[0][0][1], v0);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int c = 0; c < 2 * NB; ++c) {
+        acc[c % NB] = mma_32x32x16(f, pf[c / NB], acc[c % NB]);
+        if (c == 0) v_words(vn, 1, w[1]);
+        if (c + 1 < 2 * NB) {
+          const int p = (c + 1) / NB, b = (c + 1) % NB;
+          cvt8(f, w[p][b][0], p ? v1 : v0, w[p][b][1], p ? v1 : v0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      fetch_v(n + 2, vn);
+    };
+    // (a way out between the two steps would meet the loop's head, as the
+    // compiler lays it out, and make that wait for every load under way)
+    int n = 0;
+    for (; n + 1 < cnt; n += 2) {
+      step(n, kq[0], vq[0]);
+      step(n + 1, kq[1], vq[1]);
+    }
+    if (n < cnt) step(n, kq[0], vq[0]);
+  }
+
+  // the other tiles: those that some row does not see whole, and, after the
+  // last split's share of the prefix, the segment
+  const int n_left = f0 - t0, n_pre = n_left + t1 - f1;
+  int L = 0;
+  if (bz == ns - 1 && kv.seg_pages > 0 && r.vis_words > 0)
+    L = max(0, min(min(r.seg_len[s], kv.seg_pages * 16), r.vis_words * 32));
+  const int n_gen = n_pre + ((L + 31) >> 5);
+  for (int i = (wave + NW - (f1 - f0) % NW) % NW; i < n_gen; i += NW) {
+    f32x16_t sc;
+    Frag vf[2][NB];
+    float ks[2];
+    uint32_t seen = 0;                 // bit e: key of score e
+    if (i < n_pre) {
+      const int v0 = 2 * (i < n_left ? t0 + i : f1 + i - n_left);
+      int first[2], pg[2];             // entry number and page of each half
+      float vs[2];
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        const int ap = sp.page(min(v0 + p, sp.n - 1));
+        first[p] = v0 + p < sp.n ? ap * 16 : Tp;
+        pg[p] = checked_index(ptab[ap], kv.n_pages, kv.err, kDevPage);
+        ks[p] = byte_scale(kv.k_exp[(size_t)pg[p] * Hkv + kh]) * scale;
+        vs[p] = byte_scale(kv.v_exp[(size_t)pg[p] * Hkv + kh]);
+      }
+      load_k(pg[0], pg[1], kq[0]);
+      load_v(pg[0], pg[1], vq[0]);
+      sc = scores(kq[0]);
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        uint32_t w[NB][2];
+        v_words(vq[0], p, w);
+#pragma unroll
+        for (int b = 0; b < NB; ++b) cvt8(vf[p][b], w[b][0], vs[p], w[b][1], vs[p]);
+      }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int key = first[e >> 3] + 8 * ((e >> 2) & 1) + 4 * h + (e & 3);
+        seen |= (uint32_t)((key < Tp) & ((key < r.sinks) | (key >= lo))) << e;
+      }
+    } else {
+      const int t = i - n_pre;
+      ks[0] = ks[1] = scale;
+      const int pk = min(2 * t + (c32 >> 4), kv.seg_pages - 1);
+      const bf16_t* kp = static_cast<const bf16_t*>(kv.seg_k) +
+                         (((size_t)s * kv.seg_pages + pk) * Hkv + kh) * 16 * HD +
+                         (c32 & 15) * HD + h * (HD / 2);
+      sc = zero16();
+#pragma unroll
+      for (int c = 0; c < NK; ++c) {
+        Frag kf;
+        kf.load(kp + 8 * c);
+        sc = mma_32x32x16(kf, qf[c], sc);
+      }
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        const int pv = min(2 * t + p, kv.seg_pages - 1);
+        const bf16_t* vp = static_cast<const bf16_t*>(kv.seg_v) +
+                           (((size_t)s * kv.seg_pages + pv) * Hkv + kh) * 16 * HD +
+                           c32 * 16 + 4 * h;
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          const uint2 x = *reinterpret_cast<const uint2*>(vp + 512 * b);
+          const uint2 y = *reinterpret_cast<const uint2*>(vp + 512 * b + 8);
+          vf[p][b].v = make_uint4(x.x, x.y, y.x, y.y);
+        }
+      }
+      const uint32_t word = r.vis[(size_t)row * r.vis_words + t];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int slot = 16 * (e >> 3) + 8 * ((e >> 2) & 1) + 4 * h + (e & 3);
+        seen |= (uint32_t)(((word >> slot) & 1u) & (32 * t + slot < L)) << e;
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 16; ++e) sc[e] = (seen >> e) & 1u ? sc[e] : -__builtin_inff();
+    refer(sc, ks[0], ks[1]);
+    Frag pf[2];
+#pragma unroll
+    for (int c = 0; c < 8; ++c) put(pf, c, weigh(sc[2 * c], sc[2 * c + 1]));
+    uint32_t bad = 0;
+#pragma unroll
+    for (int p = 0; p < 2; ++p)
+#pragma unroll
+      for (int b = 0; b < NB; ++b) bad |= bad_bits(vf[p][b]);
+    if (__ballot(bad != 0) != 0) {
+#pragma unroll
+      for (int p = 0; p < 2; ++p)
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          acc[b] = add_bad32(take_bad(vf[p][b]), (seen >> (8 * p)) & 0xFFu, acc[b]);
+          __builtin_amdgcn_sched_barrier(0);   // (one operand at a time)
+        }
+    }
+#pragma unroll
+    for (int p = 0; p < 2; ++p)
+#pragma unroll
+      for (int b = 0; b < NB; ++b) acc[b] = mma_32x32x16(vf[p][b], pf[p], acc[b]);
+  }
+
+  // the waves' shares
+  l = sum_x32(l);
+  if (h == 0) {
+    msh[wave][c32] = lim < 0.f ? kLow : m;
+    lsh[wave][c32] = l;
+  }
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      *reinterpret_cast<float4*>(&osh[wave][c32][32 * b + 8 * g + 4 * h]) = make_float4(
+          acc[b][4 * g], acc[b][4 * g + 1], acc[b][4 * g + 2], acc[b][4 * g + 3]);
+  __syncthreads();
+  constexpr int TPQ = NW * 64 / 32;     // threads of one query vector
+  const int qj = tid / TPQ, part = tid % TPQ, qv = q0 + qj;
+  if (qv >= nq) return;
+  float M = kLow, Lsum = 0.f, wt[NW];
+#pragma unroll
+  for (int w = 0; w < NW; ++w) M = fmaxf(M, msh[w][qj]);
+#pragma unroll
+  for (int w = 0; w < NW; ++w) {
+    wt[w] = __builtin_amdgcn_exp2f(msh[w][qj] - M);
+    Lsum += wt[w] * lsh[w][qj];
+  }
+  const int rq = div_small(qv, G);
+  const float inv = Lsum == 0.f ? 0.f : 1.0f / Lsum;
+  const size_t at = (size_t)(row0 + rq) * H + kh * G + qv - rq * G;
+#pragma unroll
+  for (int col = part * 4; col < HD; col += 4 * TPQ) {
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const float4 x = *reinterpret_cast<const float4*>(&osh[w][qj][col]);
+      o.x += wt[w] * x.x;
+      o.y += wt[w] * x.y;
+      o.z += wt[w] * x.z;
+      o.w += wt[w] * x.w;
+    }
+    if (ns > 1)
+      *reinterpret_cast<float4*>(
+          o_part + ((size_t)bz * r.n_rows * H + at) * HD + col) = o;
+    else
+      store4(out + at * HD + col, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+  }
+  if (ns > 1 && part == 0)
+    *reinterpret_cast<float2*>(ml + ((size_t)bz * r.n_rows * H + at) * 2) =
+        make_float2(M, Lsum);
 }
 
 // Rows of sequences with several splits: o = sum_z w_z O_z / sum_z w_z l_z,
@@ -610,36 +994,32 @@ __global__ __launch_bounds__(256) void kvq_merge_kernel(
     o.w += w * x.w;
   }
   const float inv = L == 0.f ? 0.f : 1.0f / L;
-  T* dst = out + row * H * hd + 4 * c;
-  if constexpr (sizeof(T) == 2)
-    *reinterpret_cast<uint2*>(dst) = make_uint2(
-        pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
-  else
-    *reinterpret_cast<float4*>(dst) =
-        make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+  store4(out + row * H * hd + 4 * c,
+         make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
 }
 
 int cdiv(long a, long b) { return (int)((a + b - 1) / b); }
 
 }  // namespace
 
-// Two query tiles a workgroup where there are more than one (a tile's codes
-// are converted once for both: 16 trees of up to 64 nodes 74 -> 49 us, a tree
-// of 512 nodes over 8192 entries 179 -> 102; four do not fit the registers: 60
-// and 128).  Enough workgroups for two on every CU, cut no shorter than 256
-// entries (60 nodes over 1024: 13.5 us, with 128 17.1); beyond that long
-// prefixes are cut to 4096 entries so that ragged batches end together.
+// 32 query vectors a workgroup where there are more than 16 of a KV head (16
+// trees of up to 64 nodes 68 us with 16, 48 with 32; fp32 has 16 throughout).
+// As many splits as give a workgroup on every CU and keep 256 entries each (60
+// nodes over 1024: 13.4 us, with 128 17.1): what a second one on a CU gains the
+// merge costs (500 rows over 8192: 94 us, in two 106; 8 windows of 4096, 33
+// rows each: 30.5, in two 38.7).  Longer prefixes are cut to 8192 entries so
+// that ragged batches end together.
 QPlan kvq_attn_plan(int n_seqs, int rows_per_seq, int max_prefix, int window,
-                    int sinks, int H, int Hkv, int hd, int es, int max_split) {
+                    int sinks, int H, int Hkv, int es, int max_split) {
   long eff = max_prefix;
   if (window > 0) eff = std::min(eff, (long)window + sinks + 32);
   const long nq = (long)rows_per_seq * (H / Hkv);
-  const int qt = es == 4 || nq <= 16 ? 1 : 2;
-  const long items = (long)cdiv(nq, 16 * qt) * n_seqs * Hkv;
-  int nz = std::min(cdiv(512, items), std::max(1, (int)(eff / 256)));
-  nz = std::max(nz, cdiv(eff, 4096));
-  nz = std::max(1, std::min({nz, max_split, kMaxSplit}));
-  return QPlan{nz, std::max(32, cdiv(cdiv(eff, nz), 32) * 32), qt};
+  const int width = es == 4 || nq <= 16 ? 16 : 32;
+  const long items = (long)cdiv(nq, width) * n_seqs * Hkv;
+  long nz = std::min(std::max(1L, 256 / items), std::max(1L, eff / 256));
+  nz = std::max<long>(nz, cdiv(eff, 8192));
+  nz = std::max(1L, std::min<long>({nz, max_split, kMaxSplit}));
+  return QPlan{(int)nz, std::max(32, cdiv(cdiv(eff, nz), 32) * 32), width};
 }
 
 template <typename T>
@@ -647,19 +1027,29 @@ void launch_kvq_attn(const T* q, const QRows& r, const QView& kv, int H,
                      int Hkv, int hd, const QPlan& plan, float* o_part,
                      float* ml, T* out, hipStream_t st) {
   const float scale = 1.0f / sqrtf((float)hd);
-  const dim3 grid(cdiv((long)r.rows_per_seq * (H / Hkv), 16 * plan.qt),
-                  r.n_seqs * Hkv, plan.n_split);
-  auto k = hd == 128 ? kvq_attn_kernel<T, 128, 1> : kvq_attn_kernel<T, 64, 1>;
-  if constexpr (sizeof(T) == 2) {
-    if (plan.qt == 2) k = hd == 128 ? kvq_attn_kernel<T, 128, 2> : kvq_attn_kernel<T, 64, 2>;
-  }
+  const int groups = cdiv((long)r.rows_per_seq * (H / Hkv), plan.width);
+  const int items = cdiv((long)r.n_seqs * Hkv * plan.n_split, 8) * 8;
+  const dim3 grid(groups * items);
   // (the profiler's events: start of this kernel, end of the last one)
   hipEvent_t ea, eb;
   attn_take_events(&ea, &eb);
   const bool merge = plan.n_split > 1;
-  hipExtLaunchKernelGGL(k, grid, dim3(kWaves * 64), 0, st, ea, merge ? nullptr : eb,
-                        0, q, r, kv, H, Hkv, plan.n_split, plan.split_tokens,
-                        scale, o_part, ml, out);
+#define SB_RUN(K_)                                                        \
+  hipExtLaunchKernelGGL(K_, grid, dim3(NW * 64), 0, st, ea, merge ? nullptr : eb, 0, \
+                        q, r, kv, groups, H, Hkv, plan.n_split,                \
+                        plan.split_tokens, scale, o_part, ml, out)
+  const bool wide = plan.width == 32;
+  if constexpr (sizeof(T) == 2) {
+    if (wide) {
+      auto k = hd == 128 ? kvq_attn32_kernel<128> : kvq_attn32_kernel<64>;
+      SB_RUN(k);
+    }
+  }
+  if (!wide) {
+    auto k = hd == 128 ? kvq_attn_kernel<T, 128> : kvq_attn_kernel<T, 64>;
+    SB_RUN(k);
+  }
+#undef SB_RUN
   if (merge)
     hipExtLaunchKernelGGL(kvq_merge_kernel<T>,
                           dim3(cdiv(H * hd, 1024), r.rows_per_seq, r.n_seqs),
