@@ -199,6 +199,16 @@ __device__ __forceinline__ void rows_of(const QRows& r, int s, int& row0, int& n
   const int row1 = max(row0, min(r.row_off[s + 1], r.n_rows));
   n = min(row1 - row0, r.rows_per_seq);
 }
+// Keys first .. first + 15 that a row sees, a bit each: below T, and below the
+// sinks or from lo on.
+__device__ __forceinline__ uint32_t page_bits(int first, int T, int sinks, int lo) {
+  auto below = [&](int x) { return (1u << min(max(x - first, 0), 16)) - 1u; };
+  return below(T) & (below(sinks) | ~below(lo));
+}
+// Segment slots 32 t .. 32 t + 31 that a row sees, of L > 32 t.
+__device__ __forceinline__ uint32_t slot_bits(uint32_t word, int t, int L) {
+  return L - 32 * t >= 32 ? word : word & ((1u << (L - 32 * t)) - 1u);
+}
 __device__ __forceinline__ int wave_max_i(int v) { return -wave_min_i(-v); }
 
 // What a workgroup works on.  The dispatcher deals workgroups out round-robin
@@ -387,20 +397,28 @@ sc[h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     L = max(0, min(min(r.seg_len[s], kv.seg_pages * 16), r.vis_words * 32));
   const int n_gen = n_pre + ((L + 31) >> 5);
   for (int i = (wave + NW - (f1 - f0) % NW) % NW; i < n_gen; i += NW) {
+    // which keys of the tile the row sees
+    uint32_t keys;
+    const int v0 = 2 * (i < n_left ? t0 + i : f1 + i - n_left), t = i - n_pre;
+    if (i < n_pre) {
+      keys = page_bits(sp.page(v0) * 16, Tp, r.sinks, lo);
+      if (v0 + 1 < sp.n) keys |= page_bits(sp.page(v0 + 1) * 16, Tp, r.sinks, lo) << 16;
+    } else {
+      keys = slot_bits(r.vis[(size_t)row * r.vis_words + t], t, L);
+    }
+    if (__ballot(keys != 0) == 0) continue;
+    keys >>= 4 * g;
+    const uint32_t seen = (keys & 15) | ((keys >> 12) & 0xF0);   // bit e: key of score e
     Frag8<T> vf[NC];
     f32x4_t sc[2];
     float ks[2];
-    uint32_t seen = 0;                 // bit e: key of score e
     sc[0] = sc[1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     if (i < n_pre) {
-      const int v0 = 2 * (i < n_left ? t0 + i : f1 + i - n_left);
-      int first[2];                    // entry number of each half
       uint4 kd[2][W4], vd[2][W4];
       float vs[2];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int ap = sp.page(min(v0 + h, sp.n - 1));
-        first[h] = v0 + h < sp.n ? ap * 16 : Tp;
         const int pg = checked_index(ptab[ap], kv.n_pages, kv.err, kDevPage);
         load_page(pg, kd[h], vd[h]);
         ks[h] = byte_scale(kv.k_exp[(size_t)pg * Hkv + kh]) * scale;
@@ -420,13 +438,7 @@ sc[h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
       const uint32_t* w1 = reinterpret_cast<const uint32_t*>(&vd[1][0]);
 #pragma unroll
       for (int c = 0; c < NC; ++c) cvt8(vf[c], w0[c], vs[0], w1[c], vs[1]);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int key = first[e >> 2] + 4 * g + (e & 3);
-        seen |= (uint32_t)(key < Tp && (key < r.sinks || key >= lo)) << e;
-      }
     } else {
-      const int t = i - n_pre;
       const T* kp[2];
       const T* vp[2];
 #pragma unroll
@@ -453,12 +465,6 @@ sc[h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
           vf[c].a = *reinterpret_cast<const float4*>(vp[0] + 256 * c);
           vf[c].b = *reinterpret_cast<const float4*>(vp[1] + 256 * c);
         }
-      }
-      const uint32_t word = r.vis[(size_t)row * r.vis_words + t];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int slot = 16 * (e >> 2) + 4 * g + (e & 3);
-        seen |= (uint32_t)(((word >> slot) & 1u) && 32 * t + slot < L) << e;
       }
     }
 #pragma unroll
@@ -819,18 +825,29 @@ __global__ __launch_bounds__(NW * 64, 2) void kvq_attn32_kernel(
     L = max(0, min(min(r.seg_len[s], kv.seg_pages * 16), r.vis_words * 32));
   const int n_gen = n_pre + ((L + 31) >> 5);
   for (int i = (wave + NW - (f1 - f0) % NW) % NW; i < n_gen; i += NW) {
+    // which keys of the tile the row sees
+    uint32_t keys;
+    const int v0 = 2 * (i < n_left ? t0 + i : f1 + i - n_left), t = i - n_pre;
+    if (i < n_pre) {
+      keys = page_bits(sp.page(v0) * 16, Tp, r.sinks, lo);
+      if (v0 + 1 < sp.n) keys |= page_bits(sp.page(v0 + 1) * 16, Tp, r.sinks, lo) << 16;
+    } else {
+      keys = slot_bits(r.vis[(size_t)row * r.vis_words + t], t, L);
+    }
+    if (__ballot(keys != 0) == 0) continue;
+    keys >>= 4 * h;
+    // bit e: key of score e
+    const uint32_t seen = (keys & 15) | ((keys >> 4) & 0xF0) | ((keys >> 8) & 0xF00) |
+                          ((keys >> 12) & 0xF000);
     f32x16_t sc;
     Frag vf[2][NB];
     float ks[2];
-    uint32_t seen = 0;                 // bit e: key of score e
     if (i < n_pre) {
-      const int v0 = 2 * (i < n_left ? t0 + i : f1 + i - n_left);
-      int first[2], pg[2];             // entry number and page of each half
+      int pg[2];
       float vs[2];
 #pragma unroll
       for (int p = 0; p < 2; ++p) {
         const int ap = sp.page(min(v0 + p, sp.n - 1));
-        first[p] = v0 + p < sp.n ? ap * 16 : Tp;
         pg[p] = checked_index(ptab[ap], kv.n_pages, kv.err, kDevPage);
         ks[p] = byte_scale(kv.k_exp[(size_t)pg[p] * Hkv + kh]) * scale;
         vs[p] = byte_scale(kv.v_exp[(size_t)pg[p] * Hkv + kh]);
@@ -845,13 +862,7 @@ __global__ __launch_bounds__(NW * 64, 2) void kvq_attn32_kernel(
 #pragma unroll
         for (int b = 0; b < NB; ++b) cvt8(vf[p][b], w[b][0], vs[p], w[b][1], vs[p]);
       }
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int key = first[e >> 3] + 8 * ((e >> 2) & 1) + 4 * h + (e & 3);
-        seen |= (uint32_t)((key < Tp) & ((key < r.sinks) | (key >= lo))) << e;
-      }
     } else {
-      const int t = i - n_pre;
       ks[0] = ks[1] = scale;
       const int pk = min(2 * t + (c32 >> 4), kv.seg_pages - 1);
       const bf16_t* kp = static_cast<const bf16_t*>(kv.seg_k) +
@@ -876,12 +887,6 @@ __global__ __launch_bounds__(NW * 64, 2) void kvq_attn32_kernel(
           const uint2 y = *reinterpret_cast<const uint2*>(vp + 512 * b + 8);
           vf[p][b].v = make_uint4(x.x, x.y, y.x, y.y);
         }
-      }
-      const uint32_t word = r.vis[(size_t)row * r.vis_words + t];
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int slot = 16 * (e >> 3) + 8 * ((e >> 2) & 1) + 4 * h + (e & 3);
-        seen |= (uint32_t)(((word >> slot) & 1u) & (32 * t + slot < L)) << e;
       }
     }
 #pragma unroll
@@ -1004,11 +1009,13 @@ int cdiv(long a, long b) { return (int)((a + b - 1) / b); }
 
 // 32 query vectors a workgroup where there are more than 16 of a KV head (16
 // trees of up to 64 nodes 68 us with 16, 48 with 32; fp32 has 16 throughout).
-// As many splits as give a workgroup on every CU and keep 256 entries each (60
-// nodes over 1024: 13.4 us, with 128 17.1): what a second one on a CU gains the
-// merge costs (500 rows over 8192: 94 us, in two 106; 8 windows of 4096, 33
-// rows each: 30.5, in two 38.7).  Longer prefixes are cut to 8192 entries so
-// that ragged batches end together.
+// No split below 1280 entries, where the merge costs what it saves (a row over
+// 512: 7.2 us, in two 9.4; 60 nodes over 1024: 12.4, in four 13.2; over 1536:
+// 14.9, in six 13.6).  Beyond that as many as give a workgroup on every CU and
+// keep 256 entries each, of more than eight 512 (a row over 8192: 14.0 us in 16,
+// 16.6 in 32): what a second one on a CU gains the merge costs (500 rows over
+// 8192: 94 us, in two 106; 8 windows of 4096, 33 rows each: 30.5, in two 38.7).
+// Longer prefixes are cut to 8192 entries so that ragged batches end together.
 QPlan kvq_attn_plan(int n_seqs, int rows_per_seq, int max_prefix, int window,
                     int sinks, int H, int Hkv, int es, int max_split) {
   long eff = max_prefix;
@@ -1016,7 +1023,9 @@ QPlan kvq_attn_plan(int n_seqs, int rows_per_seq, int max_prefix, int window,
   const long nq = (long)rows_per_seq * (H / Hkv);
   const int width = es == 4 || nq <= 16 ? 16 : 32;
   const long items = (long)cdiv(nq, width) * n_seqs * Hkv;
-  long nz = std::min(std::max(1L, 256 / items), std::max(1L, eff / 256));
+  long nz = 1;
+  if (eff >= 1280)
+    nz = std::min(std::max(1L, 256 / items), std::min(eff / 256, std::max(8L, eff / 512)));
   nz = std::max<long>(nz, cdiv(eff, 8192));
   nz = std::max(1L, std::min<long>({nz, max_split, kMaxSplit}));
   return QPlan{(int)nz, std::max(32, cdiv(cdiv(eff, nz), 32) * 32), width};
