@@ -1027,7 +1027,8 @@ QPlan kvq_attn_plan(int n_seqs, int rows_per_seq, int max_prefix, int window,
   if (eff >= 1280)
     nz = std::min(std::max(1L, 256 / items), std::min(eff / 256, std::max(8L, eff / 512)));
   nz = std::max<long>(nz, cdiv(eff, 8192));
-  nz = std::max(1L, std::min<long>({nz, max_split, kMaxSplit}));
+  // (the last bound: a launch holds fewer than 2^32 threads)
+  nz = std::max(1L, std::min<long>({nz, max_split, kMaxSplit, (1L << 23) / items}));
   return QPlan{(int)nz, std::max(32, cdiv(cdiv(eff, nz), 32) * 32), width};
 }
 

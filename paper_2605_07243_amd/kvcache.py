@@ -25,6 +25,14 @@ def _tensor(t, name, dtype, shape, device=None):
     return C.c_void_p(t.data_ptr())
 
 
+def int32(x, name, least=0):
+    """x as an int32 argument (ctypes would cut it to its low bits)."""
+    x = int(x)
+    if not least <= x < 1 << 31:
+        raise ValueError(f"{name} must be in {least} .. 2^31 - 1")
+    return x
+
+
 # handle of the current stream of a device (the integer alone: building a
 # torch.cuda.Stream for it costs as much as the rest of a call)
 _stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
@@ -102,7 +110,7 @@ class QuantKV:
     def store(self, src, first, last, max_entries):
         """Entries first[s] .. last[s] - 1 of ``src`` (a PagedKV) into this
         cache; first, last: int32 tensors [n_seqs]."""
-        n = first.shape[0]
+        n, most = first.shape[0], int32(max_entries, "max_entries", 1)
         if src.shape.dtype != self.shape.dtype or src.device != self.device or (
                 src.shape.n_kv_heads, src.shape.head_dim, src.shape.max_seqs,
                 src.shape.max_pages) != (self.shape.n_kv_heads, self.shape.head_dim,
@@ -111,7 +119,7 @@ class QuantKV:
         a = _tensor(first, "first", torch.int32, (n,), self.device)
         z = _tensor(last, "last", torch.int32, (n,), self.device)
         _call(self.device, self.lib.sb_kvq_store, self.shape.c, n, src.c, a, z,
-              int(max_entries), self.c)
+              most, self.c)
 
 
 class Attention:
@@ -125,7 +133,13 @@ class Attention:
                  window=0, sinks=0):
         sh, dev = cache.shape, cache.device
         self.lib, self.cache, self.device = B.load(), cache, dev
-        self.n_rows, self.window, self.sinks = n_rows, window, sinks
+        self.n_rows = n_rows = int32(n_rows, "n_rows", 1)
+        self.window, self.sinks = int32(window, "window"), int32(sinks, "sinks")
+        rows_per_seq = int32(rows_per_seq, "rows_per_seq", 1)
+        max_prefix = int32(max_prefix, "max_prefix")
+        given = [t is not None for t in (seg_len, vis, seg_k, seg_v)]
+        if any(given) and not all(given):
+            raise ValueError("a segment needs seg_len, vis, seg_k and seg_v")
         n = row_off.shape[0] - 1
         i32 = torch.int32
         null = C.c_void_p(0)
@@ -144,7 +158,7 @@ class Attention:
             null if pos is None else _tensor(pos, "pos", i32, (n_rows,), dev),
             _tensor(prefix_len, "prefix_len", i32, (n,), dev), sl, vs, sk, sv)
         self._keep = (row_off, pos, prefix_len, seg_len, vis, seg_k, seg_v)
-        nbytes = self.lib.sb_kvq_attend_workspace(sh.c, self.rows, window, sinks)
+        nbytes = self.lib.sb_kvq_attend_workspace(sh.c, self.rows, self.window, self.sinks)
         if nbytes == 0:
             raise B.SBError(B.SB_ESHAPE, self.lib.sb_last_error(None).decode())
         self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
@@ -208,8 +222,10 @@ class PagePool:
         for c in caches:
             if c.page_table.data_ptr() != self.page_table.data_ptr():
                 raise ValueError("the cache goes through another page table")
-            if (c.shape.n_kv_heads, c.shape.head_dim, c.shape.dtype) != (
-                    self.shape.n_kv_heads, self.shape.head_dim, self.shape.dtype):
+            if (c.shape.n_kv_heads, c.shape.head_dim, c.shape.dtype,
+                    c.shape.max_seqs, c.shape.max_pages) != (
+                    self.shape.n_kv_heads, self.shape.head_dim, self.shape.dtype,
+                    self.shape.max_seqs, self.shape.max_pages):
                 raise ValueError("the cache has another shape")
         self._caches = list(caches)
         self._kv = kv[0].c if kv else None
@@ -221,9 +237,9 @@ class PagePool:
     def grow(self, length, extra=0):
         """Pages for length[s] + extra entries of sequences 0 .. n - 1
         (length: int32 tensor [n])."""
-        n = length.shape[0]
+        n, extra = length.shape[0], int32(extra, "extra")
         _call(self.device, self.lib.sb_pool_grow, self.shape.c, self.c, n,
-              _tensor(length, "length", torch.int32, (n,), self.device), int(extra))
+              _tensor(length, "length", torch.int32, (n,), self.device), extra)
 
     def release(self, seqs):
         """The listed sequences return what they hold."""

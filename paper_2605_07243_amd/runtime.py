@@ -56,6 +56,10 @@ class Runtime:
                  adapt_cap=0, share_layers=False, prefill_rows=2048, kvq=False,
                  window=0, sinks=0):
         self.lib = B.load()
+        if not kvq and (window or sinks):
+            raise ValueError("window and sinks belong to the 8-bit cache (kvq)")
+        self.window, self.sinks = (kvcache.int32(window, "window"),
+                                   kvcache.int32(sinks, "sinks"))
         self.w = w
         self.dev = torch.device(device)
         s = w.target
@@ -97,7 +101,6 @@ class Runtime:
         B.check(self.lib, ctx, self.lib.sb_bind(
             ctx, C.byref(self.tw_c), C.byref(self.dw_c),
             _ptr(self.workspace), nbytes))
-        self.window, self.sinks = window, sinks
         self.kvq = self.pool = None
         self._buffers(page_seed)
         if kvq:

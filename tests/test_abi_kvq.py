@@ -1,10 +1,14 @@
 """Host-side checks of the 8-bit cache's and the page pool's entry points: what
 is refused, with which code and message, before anything is enqueued.  No GPU."""
 import ctypes as C
+import types
 
 import pytest
+import torch
 
 from paper_2605_07243_amd import binding as B
+from paper_2605_07243_amd import kvcache
+from paper_2605_07243_amd.runtime import Runtime
 from test_abi import Fake, bound, cfg, lib  # noqa: F401
 
 
@@ -237,3 +241,49 @@ def test_unbound_context(lib):  # noqa: F811
     assert lib.sb_commit_kvq(ctx, C.byref(sq), C.byref(t), C.byref(out), C.byref(acc),
                              kvq(f), kv(f, n_layers=1), None) == B.SB_ESTATE
     lib.sb_destroy(ctx)
+
+
+PAST = [2 ** 31, 2 ** 32, -1]
+
+
+@pytest.mark.parametrize("name", ["window", "sinks", "max_prefix", "n_rows", "rows_per_seq"])
+@pytest.mark.parametrize("value", PAST)
+def test_handles_refuse_what_int32_does_not_hold(name, value):
+    """Values that would reach the library as their low 32 bits."""
+    sh = kvcache.Shape(8, 2, 64, "bf16", 4, 10)
+    cache = types.SimpleNamespace(shape=sh, device=torch.device("cpu"))
+    z = torch.zeros(3, dtype=torch.int32)
+    args = dict(n_rows=1, rows_per_seq=1, max_prefix=0, window=0, sinks=0)
+    args[name] = value
+    with pytest.raises(ValueError, match=name):
+        kvcache.Attention(cache, z, None, z[:2], **args)
+
+
+@pytest.mark.parametrize("value", PAST)
+def test_stores_and_grows_refuse_what_int32_does_not_hold(value):
+    z = torch.zeros(2, dtype=torch.int32)
+    store = kvcache.QuantKV.__new__(kvcache.QuantKV)
+    with pytest.raises(ValueError, match="max_entries"):
+        store.store(None, z, z, value)
+    pool = kvcache.PagePool.__new__(kvcache.PagePool)
+    with pytest.raises(ValueError, match="extra"):
+        pool.grow(z, value)
+
+
+@pytest.mark.parametrize("left_out", ["seg_len", "vis", "seg_k", "seg_v"])
+def test_a_segment_is_given_whole(left_out):
+    sh = kvcache.Shape(8, 2, 64, "bf16", 4, 10)
+    cache = types.SimpleNamespace(shape=sh, device=torch.device("cpu"))
+    z = torch.zeros(3, dtype=torch.int32)
+    seg = dict(seg_len=z, vis=z, seg_k=z, seg_v=z)
+    seg[left_out] = None
+    with pytest.raises(ValueError, match="segment"):
+        kvcache.Attention(cache, z, None, z[:2], n_rows=1, rows_per_seq=1, **seg)
+
+
+def test_a_window_needs_the_8_bit_cache():
+    for kw in (dict(window=8), dict(sinks=2)):
+        with pytest.raises(ValueError, match="8-bit"):
+            Runtime(None, **kw)
+    with pytest.raises(ValueError, match="window"):
+        Runtime(None, kvq=True, window=2 ** 32)

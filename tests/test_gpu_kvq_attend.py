@@ -159,6 +159,28 @@ def test_long_prefixes_take_splits(dtype, H, Hkv, hd, T, rows):
     c.check(c.run(max_prefix=0), rows=sample)
 
 
+@pytest.mark.parametrize("dtype,H,Hkv,hd", SHAPES[:1] + SHAPES[-1:])
+@pytest.mark.parametrize("T,rows", [([1279], [3]), ([1280], [3]), ([1281, 0, 16], [20, 1, 5]),
+                                    ([1535, 1300], [1, 9]), ([2047, 255, 256, 257],
+                                                             [9, 1, 2, 17])])
+def test_lengths_where_splits_begin(dtype, H, Hkv, hd, T, rows):
+    """Around the shortest prefix that is split, beside sequences that are
+    shorter than one split."""
+    c = Case(dtype, H, Hkv, hd, T, rows, seed=14)
+    print("[attend]", dtype, T, rows, flush=True)
+    c.check(c.run())
+
+
+def test_rows_that_see_none_of_a_split():
+    """Windows that lie in one split, masks that hide whole segment tiles."""
+    c = Case("bf16", 8, 2, 128, [3000], [70], seed=15, window=40, sinks=3)
+    c.pos[:35] = 500 + np.arange(35)
+    c.vis[1::2] = 0                 # every other row: no segment slot
+    c.vis[0, :] = 0
+    c.vis[0, 2] = 1 << 5            # a slot of the last tile alone
+    c.check(c.run())
+
+
 @pytest.mark.parametrize("dtype,H,Hkv,hd", [SHAPES[0], SHAPES[4]])
 @pytest.mark.parametrize("window,sinks", [(1, 0), (1, 1), (7, 4), (16, 0), (40, 17),
                                           (100, 3), (2 ** 31 - 1, 2 ** 31 - 1),
