@@ -13,7 +13,7 @@
 // contiguous runs (K: 1 KiB per instruction; V: lane (a, r) reads slots 4 a ..
 // 4 a + 3 of column 16 c + r, 512 B per instruction for bf16), and V's stores
 // are hd / 4 consecutive bytes a lane.  16 prompts of 512 to 2048 entries in 8
-// layers of 8 x 128 heads: 190-200 us, 5.0 to 5.3 TB/s.  The few entries of one
+// layers of 8 x 128 heads: 183-208 us, 4.8 to 5.5 TB/s.  The few entries of one
 // iteration (16 sequences, 32 layers) take 12.8 us: a launch and the chain
 // bounds -> page -> scale and codes, each step a trip to memory.
 #include <algorithm>
