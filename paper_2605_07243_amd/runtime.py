@@ -397,6 +397,8 @@ class Runtime:
     def fork(self, parents, children):
         """Sequences children[i] become continuations of parents[i] from their
         present state (kvq only): full pages shared, the last one copied."""
+        if self.pool is None:
+            raise ValueError("forks need the 8-bit cache (kvq)")
         self.pool.fork(parents, children, self.T)
         a = torch.tensor(list(parents), device=self.dev)
         b = torch.tensor(list(children), device=self.dev)

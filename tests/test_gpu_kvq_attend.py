@@ -171,6 +171,16 @@ def test_lengths_where_splits_begin(dtype, H, Hkv, hd, T, rows):
     c.check(c.run())
 
 
+@pytest.mark.parametrize("dtype,H,Hkv,hd", SHAPES[:1] + SHAPES[-1:])
+def test_sequences_without_rows(dtype, H, Hkv, hd):
+    """A padded batch: sequences that have no rows, between and after those
+    that do, with split prefixes and without."""
+    for T in ([40, 100, 0, 7], [1500, 2000, 0, 1300]):
+        c = Case(dtype, H, Hkv, hd, T, [4, 0, 3, 0], seed=16)
+        print("[attend]", dtype, T, flush=True)
+        c.check(c.run())
+
+
 def test_rows_that_see_none_of_a_split():
     """Windows that lie in one split, masks that hide whole segment tiles."""
     c = Case("bf16", 8, 2, 128, [3000], [70], seed=15, window=40, sinks=3)

@@ -15,6 +15,7 @@ import torch
 import kvq_ref as ref
 import synth
 from gpu_harness import host, models, rel_err, runtime
+from paper_2605_07243_amd import binding as B
 
 pytestmark = [pytest.mark.gpu, pytest.mark.timeout(600)]
 
@@ -205,3 +206,37 @@ def test_the_element_type_cache_is_as_it_was():
             assert np.array_equal(x, y)
         n = int(a.tree["n_nodes"][s])
         assert np.array_equal(host(a.tree["token"])[s, :n], host(b.tree["token"])[s, :n])
+
+
+def test_out_of_range_pages_are_reported():
+    """With debug on, verification and commit report page-table entries that
+    they clamped; with valid ones nothing."""
+    w = workload("bf16", 2, 70, 40)
+    weights, _, _ = models(w)
+    rt = runtime(w, weights, max_pages=10, kvq=True)
+    rt.set_debug(True)
+    rt.prefill(synth.prompts(w))
+    rt.iteration()
+    rt.device_check()
+    for m in range(1, w.M + 1):
+        rt.expand(m)
+    saved = rt.tpt.clone()
+    rt.tpt[0, 0] = rt.kvq.k.shape[1] + 5
+    rt.tpt[1, 1] = -1
+    print("[debug] verify over out-of-range page-table entries", flush=True)
+    rt.verify()
+    with pytest.raises(B.SBError) as e:
+        rt.device_check()
+    assert e.value.code == B.SB_EDEVICE and "page" in str(e.value)
+    rt.tpt.copy_(saved)
+    rt.verify()
+    rt.accept()
+    rt.commit()
+    rt.device_check()
+
+
+def test_forks_need_the_8_bit_cache():
+    w = workload("f32", 2, 20, 17)
+    weights, _, _ = models(w)
+    with pytest.raises(ValueError, match="8-bit"):
+        runtime(w, weights, max_pages=10).fork([0], [1])
