@@ -47,6 +47,7 @@ struct QPlan {
   int n_split;
   int split_tokens;
   int width;                 // query vectors per workgroup: 16 or 32
+  int n_waves;               // waves of a workgroup
 };
 QPlan kvq_attn_plan(int n_seqs, int rows_per_seq, int max_prefix, int window,
                     int sinks, int H, int Hkv, int es, int max_split);

@@ -26,7 +26,7 @@
 // What bounds it.  Single tokens: the codes' way from HBM (64 sequences of 4096
 // to 32768 entries: 2.4 GB in 430-445 us, 5.6 TB/s; a streaming read reaches
 // 6.8).  Trees: every 32 query vectors read all of their KV head's codes from
-// L2 and convert them; 500 rows over 8192 entries take 90 us (640 TFLOP/s; 68
+// L2 and convert them; 500 rows over 8192 entries take 90 us (640 TFLOP/s; 70
 // without the loads, 49 for the products alone at a large bf16 product's rate).
 // Short prefixes: launch and the chain row bounds -> page table -> codes (a row
 // over 1024 entries 9.4 us, of which an empty launch is 5).
@@ -46,7 +46,6 @@ namespace {
 // finite, so that exp2(score - reference) of a hidden key (-inf) is 0
 constexpr float kLow = -3.0e38f;
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int NW = 4;         // waves of a workgroup
 constexpr int kMaxSplit = 64;
 
 __device__ __forceinline__ float byte_scale(int b) {
@@ -243,10 +242,11 @@ __device__ __forceinline__ Item item_of(int groups, int n_seqs, int Hkv) {
 // queries and takes every NW-th tile of 32 keys (no barrier in the loop), one
 // tile of loads ahead; their (O, m, l) meet in LDS at the end.
 template <typename T, int HD>
-__global__ __launch_bounds__(NW * 64, 2) void kvq_attn_kernel(
+__global__ __launch_bounds__(256, 2) void kvq_attn_kernel(
     const T* __restrict__ q, QRows r, QView kv, int groups, int H, int Hkv,
     int n_split, int split_tokens, float scale, float* __restrict__ o_part,
     float* __restrict__ ml, T* __restrict__ out) {
+  constexpr int NW = 4;                // waves of a workgroup
   constexpr int NK = HD / 32;          // contraction steps of a score
   constexpr int NC = HD / 16;          // output column blocks
   constexpr int W4 = HD / 64;          // 16-byte loads per page half
@@ -557,14 +557,18 @@ sc[h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 // and 8 + 4 h .. of each page, the B operand of O^T += V^T P^T.  A operand: the
 // codes of those keys for columns 32 b + r, i.e. groups a = h and 2 + h of the
 // V page; lanes r and r + 16 each load half of the 16 columns' run and swap the
-// words that the other needs (v_permlane16_swap).
+// words that the other needs (v_permlane16_swap).  K is loaded a KiB at a time and
+// turned to rows in LDS, each wave its own tiles: with the lanes 64 bytes apart, as
+// the operand has them, the loads of K alone took 73 of 90 us (500 rows over 8192
+// entries; V's 32).
 //
 // A workgroup: 32 query vectors of one KV head, one split; its NW waves take
 // every NW-th tile, as above.  Two waves a SIMD (the accumulators, the queries
-// and two tiles of loads fill the registers).  Measured beside it (500 rows over
-// 8192 entries, 90 us): 16 query vectors a wave 171, 64 a wave 94 to 108, four
-// waves of other queries on the same tiles 118, tiles converted once for four
-// such waves and shared in LDS 101.
+// and two tiles of loads fill the registers).  Bound inside the CU: the same 500
+// rows take 90 us, 48 with the loads alone and 70 without them.  Measured beside it:
+// 16 query vectors a wave 171, 64 a wave 94 to 108, four waves of other queries on
+// the same tiles 118, tiles converted once for four such waves and shared in LDS
+// 101.
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
@@ -598,7 +602,7 @@ __device__ __forceinline__ f32x16_t add_bad32(const BadParts<bf16_t>& b,
   return acc;
 }
 
-template <int HD>
+template <int HD, int NW>
 __global__ __launch_bounds__(NW * 64, 2) void kvq_attn32_kernel(
     const bf16_t* __restrict__ q, QRows r, QView kv, int groups, int H, int Hkv,
     int n_split, int split_tokens, float scale, float* __restrict__ o_part,
@@ -697,31 +701,49 @@ __global__ __launch_bounds__(NW * 64, 2) void kvq_attn32_kernel(
     if (c % 4 == 3) f.v.w = w;
   };
 
-  // a lane's codes: half a K row of the tile, and of each page of V half the
-  // words of groups h and 2 + h
+  // a lane's codes: of K 16 bytes of every KiB of the tile (or, after LDS, half
+  // a row), of each page of V half the words of groups h and 2 + h
   typedef u32x4 KRaw[HD / 32];
   typedef vword VRaw[2][2];
   const size_t page_bytes = (size_t)Hkv * 16 * HD;
   const uint8_t* kbase = kv.k + (size_t)kh * 16 * HD;
   const uint8_t* vbase = kv.v + (size_t)kh * 16 * HD;
-  const uint32_t klane = (c32 & 15) * HD + h * (HD / 2);
   const uint32_t vlane = (h * 16 + (c32 & 15)) * (HD / 4) + (c32 >> 4) * (HD / 8);
+  constexpr int NKL = HD / 32, NVL = 4;   // loads of a K tile, of a V tile
+  auto load_k1 = [&](int p0, int p1, int j, KRaw& kq) {
+    constexpr int N = HD / 64;         // 1 KiB runs of a page
+    kq[j] = *reinterpret_cast<const u32x4*>(
+        kbase + (size_t)(j < N ? p0 : p1) * page_bytes + (j % N * 1024 + lane * 16));
+  };
   auto load_k = [&](int p0, int p1, KRaw& kq) {
-    const uint8_t* b0 = kbase + (size_t)p0 * page_bytes;
-    const uint8_t* b1 = kbase + (size_t)p1 * page_bytes;
-    const uint8_t* kp = (c32 < 16 ? b0 : b1) + klane;
+#pragma unroll
+    for (int j = 0; j < NKL; ++j) load_k1(p0, p1, j, kq);
+  };
+  // a K tile goes through LDS to the lanes that need its rows (the wave's own
+  // 8 KiB, two tiles): 16-byte chunk c of row r at chunk c ^ r % NC of the row,
+  // eight lanes on different banks both ways
+  constexpr int NC = HD / 16;          // chunks of a row
+  uint8_t* ring = reinterpret_cast<uint8_t*>(&osh[wave][0][0]);
+  const int pr = lane / NC, put_at = pr * HD + ((lane % NC) ^ (pr % NC)) * 16;
+  const int get_at = c32 * HD + ((h * (NC / 2)) ^ (c32 % NC)) * 16;
+  auto put_k = [&](const KRaw& kq, int slot) {
 #pragma unroll
     for (int j = 0; j < HD / 32; ++j)
-      kq[j] = *reinterpret_cast<const u32x4*>(kp + 16 * j);
+      *reinterpret_cast<u32x4*>(ring + slot * 32 * HD + j * 1024 + put_at) = kq[j];
+    wave_lds_sync();
+  };
+  auto get_k = [&](int slot, KRaw& kq) {
+#pragma unroll
+    for (int j = 0; j < HD / 32; ++j)
+      kq[j] = *reinterpret_cast<const u32x4*>(ring + slot * 32 * HD + (get_at ^ (16 * j)));
+  };
+  auto load_v1 = [&](int p0, int p1, int j, VRaw& vq) {
+    const uint8_t* vp = vbase + (size_t)(j / 2 ? p1 : p0) * page_bytes;
+    vq[j / 2][j % 2] = *reinterpret_cast<const vword*>(vp + (vlane + j % 2 * 8 * HD));
   };
   auto load_v = [&](int p0, int p1, VRaw& vq) {
 #pragma unroll
-    for (int p = 0; p < 2; ++p) {
-      const uint8_t* vp = vbase + (size_t)(p ? p1 : p0) * page_bytes;
-#pragma unroll
-      for (int a = 0; a < 2; ++a)
-        vq[p][a] = *reinterpret_cast<const vword*>(vp + (vlane + a * 8 * HD));
-    }
+    for (int j = 0; j < NVL; ++j) load_v1(p0, p1, j, vq);
   };
   auto k_frag = [&](const KRaw& kq, int i, Frag& f) {
     cvt8(f, kq[i / 2][2 * (i % 2)], 1.f, kq[i / 2][2 * (i % 2) + 1], 1.f);
@@ -755,8 +777,8 @@ __global__ __launch_bounds__(NW * 64, 2) void kvq_attn32_kernel(
 
   // whole tiles, 64 of this wave's at a time: lane n holds the pages and the
   // four scale bytes of tile n.  The scores of tile n + 1 are formed beside the
-  // softmax of tile n; K of tile n + 3 and V of tile n + 2 are loaded into the
-  // registers that tile n leaves.
+  // softmax of tile n; K of tile n + 2 goes to LDS, K of tile n + 4 and V of
+  // tile n + 1 are loaded into free registers, a load beside each product.
   KRaw kq[2];
   VRaw vq[2];
   for (int n0 = 0; f0 + wave + NW * n0 < f1; n0 += 64) {
@@ -775,35 +797,44 @@ __global__ __launch_bounds__(NW * 64, 2) void kvq_attn32_kernel(
       n = min(n, cnt - 1);
       load_k(__builtin_amdgcn_readlane(id0, n), __builtin_amdgcn_readlane(id1, n), d);
     };
-    auto fetch_v = [&](int n, VRaw& d) {
-      n = min(n, cnt - 1);
-      load_v(__builtin_amdgcn_readlane(id0, n), __builtin_amdgcn_readlane(id1, n), d);
-    };
-    fetch_k(0, kq[1]);
-    fetch_k(1, kq[0]);
-    fetch_v(0, vq[0]);
-    f32x16_t sc = scores(kq[1]);
-    fetch_k(2, kq[1]);
-    __builtin_amdgcn_sched_barrier(0);   // (loads in the order of the loop)
-    fetch_v(1, vq[1]);
-    // one tile: kn holds K of tile n + 1, vn V of tile n (the barriers keep the
-    // compiler from taking the vector instructions ahead of the products)
-    auto step = [&](int n, KRaw& kn, VRaw& vn) {
+    fetch_k(0, kq[0]);
+    fetch_k(1, kq[1]);
+    load_v(__builtin_amdgcn_readlane(id0, 0), __builtin_amdgcn_readlane(id1, 0), vq[0]);
+    put_k(kq[0], 0);
+    fetch_k(2, kq[0]);
+    KRaw kf;
+    get_k(0, kf);
+    f32x16_t sc = scores(kf);
+    put_k(kq[1], 1);
+    fetch_k(3, kq[1]);
+    // one tile: kn holds K of tile n + 2, vn V of tile n, vo is free, the other
+    // slot of LDS holds K of tile n + 1 (the barriers keep the compiler from taking the vector
+    // instructions ahead of the products)
+    auto step = [&](int n, int slot, KRaw& kn, VRaw& vn, VRaw& vo) {
+      get_k(slot ^ 1, kf);
+      put_k(kn, slot);
+      const int nk = min(n + 4, cnt - 1), nv = min(n + 1, cnt - 1);
+      const int k0 = __builtin_amdgcn_readlane(id0, nk), k1 = __builtin_amdgcn_readlane(id1, nk);
+      const int v2 = __builtin_amdgcn_readlane(id0, nv), v3 = __builtin_amdgcn_readlane(id1, nv);
       const uint32_t e = __builtin_amdgcn_readlane(ex, n);
       refer(sc, byte_scale(e & 255) * scale, byte_scale((e >> 8) & 255) * scale);
       f32x16_t next = zero16();
       Frag pf[2], f;
-      k_frag(kn, 0, f);
+      k_frag(kf, 0, f);
 #pragma unroll
       for (int i = 0; i < NK; ++i) {
         next = mma_32x32x16(f, qf[i], next);
-        if (i + 1 < NK) k_frag(kn, i + 1, f);
+        if (i + 1 < NK) k_frag(kf, i + 1, f);
 #pragma unroll
         for (int c = i * (8 / NK); c < (i + 1) * (8 / NK); ++c)
           put(pf, c, weigh(sc[2 * c], sc[2 * c + 1]));
+#pragma unroll
+        for (int c = i * (NKL + NVL) / NK; c < (i + 1) * (NKL + NVL) / NK; ++c) {
+          if (c < NKL) load_k1(k0, k1, c, kn);
+          else load_v1(v2, v3, c - NKL, vo);
+        }
         __builtin_amdgcn_sched_barrier(0);
       }
-      fetch_k(n + 3, kn);
       sc = next;
       uint32_t w[2][NB][2];
       v_words(vn, 0, w[0]);
@@ -820,16 +851,15 @@ __global__ __launch_bounds__(NW * 64, 2) void kvq_attn32_kernel(
         }
         __builtin_amdgcn_sched_barrier(0);
       }
-      fetch_v(n + 2, vn);
     };
     // (a way out between the two steps would meet the loop's head, as the
     // compiler lays it out, and make that wait for every load under way)
     int n = 0;
     for (; n + 1 < cnt; n += 2) {
-      step(n, kq[0], vq[0]);
-      step(n + 1, kq[1], vq[1]);
+      step(n, 0, kq[0], vq[0], vq[1]);
+      step(n + 1, 1, kq[1], vq[1], vq[0]);
     }
-    if (n < cnt) step(n, kq[0], vq[0]);
+    if (n < cnt) step(n, 0, kq[0], vq[0], vq[1]);
   }
 
   // the other tiles: those that some row does not see whole, and, after the
@@ -869,7 +899,9 @@ __global__ __launch_bounds__(NW * 64, 2) void kvq_attn32_kernel(
       }
       load_k(pg[0], pg[1], kq[0]);
       load_v(pg[0], pg[1], vq[0]);
-      sc = scores(kq[0]);
+      put_k(kq[0], 0);
+      get_k(0, kq[1]);
+      sc = scores(kq[1]);
 #pragma unroll
       for (int p = 0; p < 2; ++p) {
         uint32_t w[NB][2];
@@ -1031,6 +1063,9 @@ int cdiv(long a, long b) { return (int)((a + b - 1) / b); }
 // 16.6 in 32): what a second one on a CU gains the merge costs (500 rows over
 // 8192: 94 us, in two 106; 8 windows of 4096, 33 rows each: 30.5, in two 38.7).
 // Longer prefixes are cut to 8192 entries so that ragged batches end together.
+// Eight waves a workgroup where there is at most one on a CU and it has 1024
+// entries (8 windows of 4096: 28.8 us, with four 31.7; 60 nodes over 16384: 31.7
+// and 33.3; with splits of 256 or 512 entries four are 2 to 6% faster).
 QPlan kvq_attn_plan(int n_seqs, int rows_per_seq, int max_prefix, int window,
                     int sinks, int H, int Hkv, int es, int max_split) {
   long eff = max_prefix;
@@ -1044,7 +1079,9 @@ QPlan kvq_attn_plan(int n_seqs, int rows_per_seq, int max_prefix, int window,
   nz = std::max<long>(nz, cdiv(eff, 8192));
   // (the last bound: a launch holds fewer than 2^32 threads)
   nz = std::max(1L, std::min<long>({nz, max_split, kMaxSplit, (1L << 23) / items}));
-  return QPlan{(int)nz, std::max(32, cdiv(cdiv(eff, nz), 32) * 32), width};
+  const int tokens = std::max(32, cdiv(cdiv(eff, nz), 32) * 32);
+  const int n_waves = width == 32 && items * nz <= 256 && tokens >= 1024 ? 8 : 4;
+  return QPlan{(int)nz, tokens, width, n_waves};
 }
 
 template <typename T>
@@ -1059,20 +1096,23 @@ void launch_kvq_attn(const T* q, const QRows& r, const QView& kv, int H,
   hipEvent_t ea, eb;
   attn_take_events(&ea, &eb);
   const bool merge = plan.n_split > 1;
-#define SB_RUN(K_)                                                        \
-  hipExtLaunchKernelGGL(K_, grid, dim3(NW * 64), 0, st, ea, merge ? nullptr : eb, 0, \
+#define SB_RUN(K_, N_)                                                         \
+  hipExtLaunchKernelGGL(K_, grid, dim3(N_), 0, st, ea, merge ? nullptr : eb, 0, \
                         q, r, kv, groups, H, Hkv, plan.n_split,                \
                         plan.split_tokens, scale, o_part, ml, out)
-  const bool wide = plan.width == 32;
+  const bool wide = plan.width == 32, eight = plan.n_waves == 8;
   if constexpr (sizeof(T) == 2) {
-    if (wide) {
-      auto k = hd == 128 ? kvq_attn32_kernel<128> : kvq_attn32_kernel<64>;
-      SB_RUN(k);
+    if (wide && eight) {
+      auto k = hd == 128 ? kvq_attn32_kernel<128, 8> : kvq_attn32_kernel<64, 8>;
+      SB_RUN(k, 512);
+    } else if (wide) {
+      auto k = hd == 128 ? kvq_attn32_kernel<128, 4> : kvq_attn32_kernel<64, 4>;
+      SB_RUN(k, 256);
     }
   }
   if (!wide) {
     auto k = hd == 128 ? kvq_attn_kernel<T, 128> : kvq_attn_kernel<T, 64>;
-    SB_RUN(k);
+    SB_RUN(k, 256);
   }
 #undef SB_RUN
   if (merge)
