@@ -20,12 +20,12 @@
 //
 // The softmax reference m moves only when a score exceeds it by 8 (in log2
 // units): the probabilities stay below 2^8 and the sums in fp32.  P is rounded
-// to bf16 for the bf16 product (2^-9 relative each, averaged over the keys);
+// to bf16 for the bf16 product (at most 2^-8 relative each, averaged over the keys);
 // its sum is taken before the rounding, in fp32.
 //
 // What bounds it.  Single tokens: the codes' way from HBM (64 sequences of 4096
-// to 32768 entries: 2.4 GB in 430-445 us, 5.6 TB/s; a streaming read reaches
-// 6.8).  Trees: every 32 query vectors read all of their KV head's codes from
+// to 32768 entries: 2.4 GB in 418-455 us, 5.3 to 5.8 TB/s; a streaming read
+// reaches 6.8).  Trees: every 32 query vectors read all of their KV head's codes from
 // L2 and convert them; 500 rows over 8192 entries take 90 us (640 TFLOP/s; 70
 // without the loads, 49 for the products alone at a large bf16 product's rate).
 // Short prefixes: launch and the chain row bounds -> page table -> codes (a row
@@ -808,8 +808,7 @@ __global__ __launch_bounds__(NW * 64, 2) void kvq_attn32_kernel(
     put_k(kq[1], 1);
     fetch_k(3, kq[1]);
     // one tile: kn holds K of tile n + 2, vn V of tile n, vo is free, the other
-    // slot of LDS holds K of tile n + 1 (the barriers keep the compiler from taking the vector
-    // instructions ahead of the products)
+    // slot of LDS holds K of tile n + 1
     auto step = [&](int n, int slot, KRaw& kn, VRaw& vn, VRaw& vo) {
       get_k(slot ^ 1, kf);
       put_k(kn, slot);
@@ -833,14 +832,13 @@ __global__ __launch_bounds__(NW * 64, 2) void kvq_attn32_kernel(
           if (c < NKL) load_k1(k0, k1, c, kn);
           else load_v1(v2, v3, c - NKL, vo);
         }
-        __builtin_amdgcn_sched_barrier(0);
       }
       sc = next;
       uint32_t w[2][NB][2];
       v_words(vn, 0, w[0]);
       const float v0 = byte_scale((e >> 16) & 255), v1 = byte_scale(e >> 24);
       cvt8(f, w[0][0][0], v0, w[0][0][1], v0);
-      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_sched_barrier(0);   // (first the softmax, then V's conversions)
 #pragma unroll
       for (int c = 0; c < 2 * NB; ++c) {
         acc[c % NB] = mma_32x32x16(f, pf[c / NB], acc[c % NB]);
@@ -849,7 +847,6 @@ __global__ __launch_bounds__(NW * 64, 2) void kvq_attn32_kernel(
           const int p = (c + 1) / NB, b = (c + 1) % NB;
           cvt8(f, w[p][b][0], p ? v1 : v0, w[p][b][1], p ? v1 : v0);
         }
-        __builtin_amdgcn_sched_barrier(0);
       }
     };
     // (a way out between the two steps would meet the loop's head, as the
