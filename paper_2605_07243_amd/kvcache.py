@@ -33,6 +33,11 @@ def int32(x, name, least=0):
     return x
 
 
+def _seqs(seqs):
+    """A host list of sequences."""
+    return (C.c_int32 * max(1, len(seqs)))(*(int32(s, "a sequence") for s in seqs))
+
+
 # handle of the current stream of a device (the integer alone: building a
 # torch.cuda.Stream for it costs as much as the rest of a call)
 _stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
@@ -164,7 +169,7 @@ class Attention:
         self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
         self._ws = C.c_void_p(self.workspace.data_ptr())
         self._rows_shape = torch.Size((n_rows, sh.n_heads, sh.head_dim))
-        self._nbytes = nbytes
+        self._nbytes, self._layers = nbytes, cache.c.n_layers
         self._attend = self.lib.sb_kvq_attend
 
     def _fits(self, t):
@@ -173,6 +178,8 @@ class Attention:
 
     def __call__(self, layer, q, out=None):
         """Attention outputs of the rows, [n_rows][n_heads][head_dim]."""
+        if not 0 <= layer < self._layers:
+            raise ValueError(f"layer must be in 0 .. {self._layers - 1}")
         if out is None:
             out = torch.empty_like(q)
         if not (self._fits(q) and self._fits(out)):
@@ -243,7 +250,7 @@ class PagePool:
 
     def release(self, seqs):
         """The listed sequences return what they hold."""
-        arr = (C.c_int32 * max(1, len(seqs)))(*seqs)
+        arr = _seqs(seqs)
         _call(self.device, self.lib.sb_pool_release, self.shape.c, self.c,
               len(seqs), arr)
 
@@ -253,8 +260,7 @@ class PagePool:
         n = len(parents)
         if len(children) != n:
             raise ValueError("as many children as parents")
-        pa = (C.c_int32 * max(1, n))(*parents)
-        ch = (C.c_int32 * max(1, n))(*children)
+        pa, ch = _seqs(parents), _seqs(children)
         _call(self.device, self.lib.sb_pool_fork, self.shape.c, self.c, n, pa, ch,
               _tensor(length, "length", torch.int32, (self.shape.max_seqs,),
                       self.device), self._kv, self._kvq)

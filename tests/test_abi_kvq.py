@@ -287,3 +287,19 @@ def test_a_window_needs_the_8_bit_cache():
             Runtime(None, **kw)
     with pytest.raises(ValueError, match="window"):
         Runtime(None, kvq=True, window=2 ** 32)
+
+
+def test_layers_and_sequences_that_int32_does_not_hold():
+    plan = kvcache.Attention.__new__(kvcache.Attention)
+    plan._layers = 3
+    for layer in (-1, 3, 2 ** 32):
+        with pytest.raises(ValueError, match="layer"):
+            plan(layer, None)
+    pool = kvcache.PagePool.__new__(kvcache.PagePool)
+    for s in PAST:
+        with pytest.raises(ValueError, match="sequence"):
+            pool.release([0, s])
+        with pytest.raises(ValueError, match="sequence"):
+            pool.fork([0], [s], None)
+        with pytest.raises(ValueError, match="sequence"):
+            pool.fork([s], [1], None)
