@@ -26,9 +26,12 @@ constexpr int kChunk = 8192;          // pages that one workgroup walks at a tim
 // scratch: number of moves; live pages per chunk; sources; targets; new number
 // of every page
 constexpr int kCounts = 16, kLists = kCounts + 256;
+// entries of a list: a compaction moves at most half of the pages, a fork copies
+// at most a page for each of 64 children (of a small pool, more than half)
+__host__ __device__ inline size_t list_ints(int n) { return n < 128 ? 64 : (size_t)n / 2; }
 __host__ __device__ inline size_t src_at() { return kLists; }
-__host__ __device__ inline size_t dst_at(int n) { return kLists + (size_t)n / 2 + 1; }
-__host__ __device__ inline size_t map_at(int n) { return kLists + 2 * ((size_t)n / 2 + 1); }
+__host__ __device__ inline size_t dst_at(int n) { return kLists + list_ints(n); }
+__host__ __device__ inline size_t map_at(int n) { return kLists + 2 * list_ints(n); }
 
 // Walks pages base .. base + kChunk - 1 with 1024 threads: fn(page, rank) for
 // each with pred(page), rank counting from `before` in page order.  Returns
