@@ -418,10 +418,11 @@ int sb_set_length_bound(sb_ctx* ctx, int32_t max_T);
  * of sb_seqs.root.  Every such read is clamped into range (page to
  * 0 .. n_pages - 1, token to 0 .. vocab - 1), so a bad value never reads or
  * writes outside the pools or the embedding table; it silently computes on
- * the clamped index instead.  sb_set_debug(ctx, 1) waits for the device,
- * clears the context's status word and makes the kernels of later calls
- * set a bit in it for every clamp (one atomic per clamped read; nothing
- * when inputs are in range); sb_set_debug(ctx, 0) stops reporting.  sb_device_check returns
+ * the clamped index instead, but for stores: a negative page-table entry names
+ * no page, and K/V that would go there are dropped.  sb_set_debug(ctx, 1) waits
+ * for the device, clears the context's status word and makes the kernels of
+ * later calls set a bit in it for every clamp or drop (one atomic per read;
+ * nothing when inputs are in range); sb_set_debug(ctx, 0) stops reporting.  sb_device_check returns
  * SB_OK at once if sb_set_debug has not been called since sb_bind (the
  * word is not cleared at bind, which touches no device memory); otherwise
  * it waits for `stream`, reads the word and, if it is not zero, clears it
@@ -548,7 +549,7 @@ int sb_profile_read_gemm(sb_ctx* ctx, sb_gemm_stat* out);
  * and more sequences (App. A.5 keeps the committed prefix on the device).
  * The calls of this part down to sb_pool_compact need no context: they take
  * the cache's shape, and their errors are in sb_last_error(NULL).  Page-table
- * entries are clamped as everywhere (see sb_set_debug); lengths, row offsets
+ * entries are treated as everywhere (see sb_set_debug); lengths, row offsets
  * and positions read on the device are cut to what the caller's buffers hold. */
 typedef struct sb_cache_shape {
   int32_t n_heads, n_kv_heads;   /* multiple of n_kv_heads, <= 64             */
@@ -577,7 +578,7 @@ typedef struct sb_kvq {
  * elem cache (written by sb_prefill, say) into an 8-bit one, each through its
  * own page table.  first, last: device [n_seqs]; max_entries: host bound of
  * last - first (entries past first + max_entries are not stored; entries
- * outside the page table neither).
+ * outside dst's page table, or where it is negative, neither).
  * Per page, KV head and K / V: e = the least integer >= -126 with
  * |x| <= 448 * 2^e for every finite value x stored by this call; when the page
  * holds earlier entries (below first) its exponent does not fall, and where it
@@ -659,7 +660,8 @@ int sb_commit_kvq(sb_ctx* ctx, sb_seqs* seqs, const sb_tree* tree,
  * calls run on the stream one after the other, never wait for the host, and
  * give the same pages whenever they are repeated from the same state. */
 typedef struct sb_pool {
-  int32_t* page_table;   /* [max_seqs][max_pages]; entries < held[s] count   */
+  int32_t* page_table;   /* [max_seqs][max_pages]; entries < held[s] count,
+                            the others are -1 (no page)                      */
   int32_t* held;         /* [max_seqs] pages that sequence s holds           */
   int32_t* refs;         /* [n_pages] sequences that hold the page           */
   int32_t* refused;      /* [1] requests that found no page or no table room */
@@ -670,13 +672,16 @@ typedef struct sb_pool {
 /* int32 values of sb_pool.scratch (0 if n_pages is invalid). */
 size_t sb_pool_scratch_ints(int32_t n_pages);
 
-/* Every page free, no sequence holding any, tables and refused 0. */
+/* Every page free, no sequence holding any, tables -1, refused 0. */
 int sb_pool_reset(const sb_cache_shape* shape, const sb_pool* pool,
                   void* stream);
 /* Sequences s < n_seqs come to hold ceil((len[s] + extra) / 16) pages (len:
  * device [n_seqs]; those that hold as many already are left), in order of s
  * the lowest free pages.  Where the pool or the table row runs out a sequence
- * holds what there was and refused counts it. */
+ * holds what there was and refused counts it: its table entries past held[s]
+ * stay -1, and what is stored there is dropped (sb_kvq_store, sb_commit_kvq).
+ * A length past 16 held[s] is the caller's to cut: the entries it lacks are
+ * lost, and reading them reads page 0. */
 int sb_pool_grow(const sb_cache_shape* shape, const sb_pool* pool,
                  int32_t n_seqs, const int32_t* len, int32_t extra,
                  void* stream);
@@ -688,7 +693,7 @@ int sb_pool_release(const sb_cache_shape* shape, const sb_pool* pool, int32_t n,
  * pages below len[parent] (device [max_seqs], cut to what the parent holds)
  * and gets a copy of its last, partly filled one in the lowest free page (in
  * order of i; refused counts a child that finds none: it holds the full pages
- * only).  kv, kvq: the caches whose pages are copied (either may be NULL),
+ * only, and its length is the caller's to cut to them).  kv, kvq: the caches whose pages are copied (either may be NULL),
  * with the pool's page table and page count. */
 int sb_pool_fork(const sb_cache_shape* shape, const sb_pool* pool, int32_t n,
                  const int32_t* parent, const int32_t* child,

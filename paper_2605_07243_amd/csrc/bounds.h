@@ -12,3 +12,11 @@ __device__ __forceinline__ int checked_index(int v, int n, int* err, int bit) {
   }
   return v;
 }
+
+// The page that a page-table entry names to a store, or -1: a negative entry
+// names none (a sequence that holds no page there), and nothing is stored
+// through it; reported as a clamp is.
+__device__ __forceinline__ int page_to_store(int v, int n, int* err, int bit) {
+  const int page = checked_index(v, n, err, bit);
+  return v < 0 ? -1 : page;
+}

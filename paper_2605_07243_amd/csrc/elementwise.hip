@@ -374,7 +374,8 @@ __global__ __launch_bounds__(256) void qkv_post_kernel(
     }
   }
   // where the row's K/V go: segment slot and / or cache entry (one outside
-  // the page table is not written: a sequence may have outgrown its table)
+  // the page table, or without a page, is not written: a sequence may have
+  // outgrown its table or its pool)
   const int seq = p.seq[i];
   T* kseg = nullptr;
   T* vseg = nullptr;
@@ -391,12 +392,14 @@ __global__ __launch_bounds__(256) void qkv_post_kernel(
   if (p.kv_row != nullptr || p.write_through) {
     const int e = p.kv_dst[i];
     if (e >= 0 && (e >> 4) < kv.max_pages) {
-      const size_t page =
-          (size_t)checked_index(kv.page_table[(size_t)seq * kv.max_pages + (e >> 4)],
-                                kv.n_pages, kv.err, kDevPage) * Hkv;
-      cl = e & 15;
-      kcache = static_cast<T*>(kv.k) + page * 16 * hd;
-      vcache = static_cast<T*>(kv.v) + page * 16 * hd;
+      const int pg = page_to_store(kv.page_table[(size_t)seq * kv.max_pages + (e >> 4)],
+                                   kv.n_pages, kv.err, kDevPage);
+      if (pg >= 0) {
+        const size_t page = (size_t)pg * Hkv;
+        cl = e & 15;
+        kcache = static_cast<T*>(kv.k) + page * 16 * hd;
+        vcache = static_cast<T*>(kv.v) + page * 16 * hd;
+      }
     }
   }
   const double pos = (double)p.pos[i];

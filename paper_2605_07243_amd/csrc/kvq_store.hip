@@ -242,8 +242,9 @@ __global__ __launch_bounds__(256) void kvq_store_kernel(Source src, sb_kvq dst,
   // slots t0 .. t1 - 1 of the page are stored, slots below t0 are held
   const int t0 = max(a - 16 * j, 0), t1 = min(z - 16 * j, 16);
   const uint32_t fresh = (t1 >= 16 ? 0xFFFFu : (1u << t1) - 1u) & ~((1u << t0) - 1u);
-  const int pg = checked_index(dst.page_table[(size_t)s * max_pages + j],
+  const int pg = page_to_store(dst.page_table[(size_t)s * max_pages + j],
                                dst.n_pages, err, kDevPage);
+  if (pg < 0) return;
   const size_t block = ((size_t)l * dst.n_pages + pg) * Hkv + kh;
   uint8_t* code = (is_v ? dst.v : dst.k) + block * 16 * HD;
   uint8_t* expo = (is_v ? dst.v_exp : dst.k_exp) + block;

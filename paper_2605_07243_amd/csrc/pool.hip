@@ -2,10 +2,12 @@
 // the copies of pages that are shared or moved.
 //
 // The state is a reference count per page (0: free) and each sequence's run of
-// page-table entries.  Free pages are given out lowest first, in the order of
-// the requests, by one workgroup that walks the counts 8192 at a time with
-// ballots: whole-number work with one result however the waves run.  Only
-// counts are added to with atomics, and sums of ones have no order.
+// page-table entries; those past the run are -1, so that nothing is stored
+// through them into a page that another sequence has.  Free pages are given out
+// lowest first, in the order of the requests, by one workgroup that walks the
+// counts 8192 at a time with ballots: whole-number work with one result however
+// the waves run.  Only counts are added to with atomics, and sums of ones have
+// no order.
 //
 // The bookkeeping is a few launches of a few microseconds (15 forks of a prompt
 // of 1003 entries in 32 layers: 17.4 us, of which the three launches are 10 and
@@ -78,7 +80,7 @@ __global__ __launch_bounds__(1024) void pool_reset_kernel(sb_pool p, int max_seq
                                                           int max_pages) {
   const size_t step = (size_t)gridDim.x * 1024;
   const size_t i0 = (size_t)blockIdx.x * 1024 + threadIdx.x;
-  for (size_t i = i0; i < (size_t)max_seqs * max_pages; i += step) p.page_table[i] = 0;
+  for (size_t i = i0; i < (size_t)max_seqs * max_pages; i += step) p.page_table[i] = -1;
   for (size_t i = i0; i < (size_t)p.n_pages; i += step) p.refs[i] = 0;
   if (i0 < (size_t)max_seqs) p.held[i0] = 0;
   if (i0 == 0) *p.refused = 0;
@@ -152,9 +154,9 @@ __global__ __launch_bounds__(1024) void pool_release_kernel(sb_pool p, PoolList 
   const int s = children ? l.b[blockIdx.x] : l.a[blockIdx.x];
   const int n = min(p.held[s], max_pages);
   for (int j = threadIdx.x; j < n; j += 1024) {
-    const int pg = checked_index(p.page_table[(size_t)s * max_pages + j], p.n_pages,
-                                 nullptr, kDevPage);
-    atomicAdd(&p.refs[pg], -1);
+    int* e = p.page_table + (size_t)s * max_pages + j;
+    atomicAdd(&p.refs[checked_index(*e, p.n_pages, nullptr, kDevPage)], -1);
+    *e = -1;
   }
   __syncthreads();
   if (threadIdx.x == 0) p.held[s] = 0;

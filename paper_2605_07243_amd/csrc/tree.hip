@@ -477,11 +477,13 @@ __global__ __launch_bounds__(512) void commit_apply_kernel(
       return;
     }
   }
-  // entries outside the page table (a negative T included) are not written
+  // entries outside the page table (a negative T included) and those that have
+  // no page are not written
   if (dst < 0 || (dst >> 4) >= kv.max_pages) return;
   const int page_i = dst >> 4;
-  const int page = checked_index(kv.page_table[(size_t)s * kv.max_pages + page_i],
+  const int page = page_to_store(kv.page_table[(size_t)s * kv.max_pages + page_i],
                                  kv.n_pages, kv.err, kDevPage);
+  if (page < 0) return;
   const int sl = dst & 15;
   const int sp = src_slot >> 4, ss = src_slot & 15;
   if (sp >= kv.seg_pages) return;

@@ -194,7 +194,10 @@ class Attention:
 
 class PagePool:
     """sb_pool over tensors, with the caches whose pages it shares and moves
-    (at most one PagedKV and one QuantKV, with the pool's page table)."""
+    (at most one PagedKV and one QuantKV, with the pool's page table).
+    page_table entries at and past held[s] are -1 (no page): what a store or a
+    commit would put there is dropped.  ``refused`` counts the requests for
+    which there was no page; a caller that may run out looks at it."""
 
     def __init__(self, shape, page_table, held, refs, refused, caches=()):
         self.lib, self.shape, self.device = B.load(), shape, page_table.device
@@ -217,7 +220,7 @@ class PagePool:
     def empty(cls, shape, n_pages, device="cuda"):
         """A pool of n_pages free pages with tables of its own."""
         z = lambda *n: torch.zeros(*n, dtype=torch.int32, device=device)  # noqa: E731
-        return cls(shape, z(shape.max_seqs, shape.max_pages), z(shape.max_seqs),
+        return cls(shape, z(shape.max_seqs, shape.max_pages) - 1, z(shape.max_seqs),
                    z(n_pages), z(1))
 
     def attach(self, caches):
@@ -243,7 +246,8 @@ class PagePool:
 
     def grow(self, length, extra=0):
         """Pages for length[s] + extra entries of sequences 0 .. n - 1
-        (length: int32 tensor [n])."""
+        (length: int32 tensor [n]); what there are of them, and refused counts
+        the sequence, when the pool or the table runs out."""
         n, extra = length.shape[0], int32(extra, "extra")
         _call(self.device, self.lib.sb_pool_grow, self.shape.c, self.c, n,
               _tensor(length, "length", torch.int32, (n,), self.device), extra)
@@ -256,7 +260,8 @@ class PagePool:
 
     def fork(self, parents, children, length):
         """children[i] continues parents[i] after length[parents[i]] entries
-        (length: int32 tensor [max_seqs])."""
+        (length: int32 tensor [max_seqs]).  A child that refused counts holds
+        the full pages alone: its length is 16 held."""
         n = len(parents)
         if len(children) != n:
             raise ValueError("as many children as parents")
