@@ -270,15 +270,17 @@ class Runtime:
         self.V = V
 
     def _quantised(self):
-        """The 8-bit target cache, and one page table and pool for it, the
-        drafter's cache and the element-type cache that prefill fills."""
+        """The 8-bit target cache, one page table and pool for it and the
+        drafter's cache, and the element-type cache that prefill fills, through
+        a table of its own (forks and compactions pass it by)."""
         s, w = self.w.target, self.w
         shape = kvcache.Shape(s.n_heads, s.n_kv_heads, s.head_dim, w.dtype,
                               self.S, self.max_pages)
         n_pages = self.tk.shape[1]
         self.pool = kvcache.PagePool.empty(shape, n_pages, self.tk.device)
-        self.tpt = self.dpt = self.pool.page_table
         self.staging = kvcache.PagedKV(shape, self.tk, self.tv, self.tpt)
+        self._staged = None     # prompt lengths, while it holds the cache's entries
+        self.tpt = self.dpt = self.pool.page_table
         self.draft_kv = kvcache.PagedKV(shape, self.dk, self.dv, self.dpt)
         self.tkv_c, self.dkv_c = self.staging.c, self.draft_kv.c
         self.kvq = kvcache.QuantKV.empty(shape, s.n_layers, n_pages, self.tpt)
@@ -309,6 +311,7 @@ class Runtime:
             C.byref(self.tkv_c), C.byref(self.dkv_c), self.stream))
         if self.kvq is not None:
             self.kvq.store(self.staging, torch.zeros_like(dlens), dlens, ld)
+            self._staged = lens
 
     def expand(self, m, want_logits=False):
         if want_logits:
@@ -375,6 +378,7 @@ class Runtime:
         vc = B.VerifyOut(_ptr(self.vout["argmax"]), _ptr(self.vout["taps"]),
                          C.c_void_p(0))
         if self.kvq is not None:
+            self._staged = None
             # pages for what this commit may add
             self.pool.grow(self.T, self.w.M * self.w.K + 1)
             self._check(self.lib.sb_commit_kvq(
@@ -400,6 +404,7 @@ class Runtime:
         if self.pool is None:
             raise ValueError("forks need the 8-bit cache (kvq)")
         self.pool.fork(parents, children, self.T)
+        self._staged = None
         a = torch.tensor(list(parents), device=self.dev)
         b = torch.tensor(list(children), device=self.dev)
         for t in (self.root, self.T, self.cond_taps):
@@ -493,14 +498,25 @@ class Runtime:
         return ((self.tk, self.tv, self.tpt) if which == "target"
                 else (self.dk, self.dv, self.dpt))
 
-    def write_cache(self, which, seq, k, v, start=0):
-        """k, v: [n_layers][n, Hkv, hd] arrays written to entries
-        start..start+n-1 of sequence seq."""
-        K_, V_, pt = self._pool(which)
-        n = np.asarray(k[0]).shape[0]
+    def _slots(self, pt, seq, n, start):
+        """Pages and slots of entries start..start+n-1 of sequence seq."""
         e = torch.arange(start, start + n, device=self.dev)
         pages = pt[seq].long()[e // 16]
-        slots = e % 16
+        if self.kvq is not None and bool((pages < 0).any()):
+            raise ValueError(f"sequence {seq} has no pages for entries "
+                             f"{start} .. {start + n - 1}")
+        return pages, e % 16
+
+    def write_cache(self, which, seq, k, v, start=0):
+        """k, v: [n_layers][n, Hkv, hd] arrays written to entries
+        start..start+n-1 of sequence seq ("drafter", or "target" without kvq:
+        an 8-bit cache is written by ``self.kvq.store``)."""
+        if which == "target" and self.kvq is not None:
+            raise ValueError("the target's cache is the 8-bit one: "
+                             "write it with kvq.store")
+        K_, V_, pt = self._pool(which)
+        n = np.asarray(k[0]).shape[0]
+        pages, slots = self._slots(pt, seq, n, start)
         for layer in range(len(k)):
             kk = torch.as_tensor(np.asarray(k[layer], np.float32)).to(self.dev)
             vv = torch.as_tensor(np.asarray(v[layer], np.float32)).to(self.dev)
@@ -508,16 +524,43 @@ class Runtime:
             V_[layer][pages, :, :, slots] = vv.to(self.et)
 
     def read_cache(self, which, seq, n, start=0):
-        """[n_layers, n, Hkv, hd] float32 copies of entries start..start+n-1."""
+        """[n_layers, n, Hkv, hd] float32 copies of entries start..start+n-1 of
+        "target" or "drafter".  With kvq "target" is what a prefill computed,
+        until the first commit or fork, and "target8" the values that the 8-bit
+        cache holds."""
+        if which == "target8":
+            return self._read_cache8(seq, n, start)
         K_, V_, pt = self._pool(which)
-        e = torch.arange(start, start + n, device=self.dev)
-        pages = pt[seq].long()[e // 16]
-        slots = e % 16
+        if which == "target" and self.kvq is not None:
+            if self._staged is None or start + n > self._staged[seq]:
+                raise ValueError(
+                    "the element-type cache holds a prefill's entries until the "
+                    'first commit or fork: read "target8"')
+            pt = self.staging.page_table
+        pages, slots = self._slots(pt, seq, n, start)
         ks = torch.stack([K_[layer][pages, :, slots, :]
                           for layer in range(K_.shape[0])])
         vs = torch.stack([V_[layer][pages, :, :, slots]
                           for layer in range(V_.shape[0])])
         return ks.float().cpu().numpy(), vs.float().cpu().numpy()
+
+    def _read_cache8(self, seq, n, start):
+        if self.kvq is None:
+            raise ValueError("there is no 8-bit cache (kvq)")
+        c, s = self.kvq, self.w.target
+        pages, slots = self._slots(self.tpt, seq, n, start)
+        out = []
+        for codes, exps, is_v in ((c.k, c.k_exp, False), (c.v, c.v_exp, True)):
+            x = codes[:, pages].view(torch.float8_e4m3fn).double()
+            x = x * torch.exp2(exps[:, pages].double() - 127)[..., None]
+            x = x.view(*x.shape[:3], *((4, 16, s.head_dim // 16, 4) if is_v
+                                       else (16, s.head_dim)))
+            if is_v:        # slot 4 a + d, column 16 c + r at [a][r][c][d]
+                x = x.permute(0, 1, 2, 3, 6, 5, 4).reshape(
+                    *x.shape[:3], 16, s.head_dim)
+            at = torch.arange(n, device=self.dev)
+            out.append(x[:, at, :, slots].transpose(0, 1).float().cpu().numpy())
+        return tuple(out)
 
     def __del__(self):
         try:
