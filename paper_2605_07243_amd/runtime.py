@@ -304,11 +304,18 @@ class Runtime:
         clens = (C.c_int32 * self.S)(*lens)
         if self.kvq is not None:
             dlens = torch.tensor(lens, dtype=torch.int32).to(self.dev)
-            self.pool.reset()
-            self.pool.grow(dlens)
-        self._check(self.lib.sb_prefill(
+            # (prompts that the library refuses leave the sequences as they are)
+            p = self.pool
+            state = [(t, t.clone()) for t in (p.page_table, p.held, p.refs, p.refused)]
+            p.reset()
+            p.grow(dlens)
+        rc = self.lib.sb_prefill(
             self.ctx, C.byref(self.seqs_c), _ptr(self.prompt_dev), ld, clens,
-            C.byref(self.tkv_c), C.byref(self.dkv_c), self.stream))
+            C.byref(self.tkv_c), C.byref(self.dkv_c), self.stream)
+        if self.kvq is not None and rc != B.SB_OK:
+            for t, was in state:
+                t.copy_(was)
+        self._check(rc)
         if self.kvq is not None:
             self.kvq.store(self.staging, torch.zeros_like(dlens), dlens, ld)
             self._staged = lens
