@@ -55,6 +55,21 @@ def _call(device, fn, *args):
         B.check(B.load(), None, rc)
 
 
+class _Scratch:
+    """Device memory that a handle allocates for the library's work, on the
+    stream that is current then."""
+
+    def __init__(self, n, dtype, device):
+        self.t = torch.empty(n, dtype=dtype, device=device)
+        self.home = _stream(device.index)
+
+    def used(self):
+        """After a call that uses it on the current stream: when the handle is
+        dropped, the memory waits for that stream too."""
+        if _stream(self.t.device.index) != self.home:
+            self.t.record_stream(torch.cuda.current_stream(self.t.device))
+
+
 class Shape:
     """sb_cache_shape: heads, element type ("bf16" or "f32") and page tables."""
 
@@ -131,7 +146,7 @@ class Attention:
     """sb_kvq_attend for one description of rows (sb_attn_rows) and one
     workspace: ``plan(layer, q, out)`` for every layer of a forward.  A plan
     runs on one stream at a time; captured graphs that may run at the same
-    time need a plan each."""
+    time need a plan each, which has to live as long as its graph."""
 
     def __init__(self, cache, row_off, pos, prefix_len, seg_len=None, vis=None,
                  seg_k=None, seg_v=None, *, n_rows, rows_per_seq, max_prefix=0,
@@ -166,7 +181,8 @@ class Attention:
         nbytes = self.lib.sb_kvq_attend_workspace(sh.c, self.rows, self.window, self.sinks)
         if nbytes == 0:
             raise B.SBError(B.SB_ESHAPE, self.lib.sb_last_error(None).decode())
-        self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+        self._scratch = _Scratch(nbytes, torch.uint8, dev)
+        self.workspace = self._scratch.t
         self._ws = C.c_void_p(self.workspace.data_ptr())
         self._rows_shape = torch.Size((n_rows, sh.n_heads, sh.head_dim))
         self._nbytes, self._layers = nbytes, cache.c.n_layers
@@ -189,6 +205,7 @@ class Attention:
         _call(self.device, self._attend, self.cache.shape.c, self.cache.c, layer,
               self.rows, q.data_ptr(), self.window, self.sinks, out.data_ptr(),
               self._ws, self._nbytes)
+        self._scratch.used()
         return out
 
 
@@ -207,7 +224,8 @@ class PagePool:
         ints = self.lib.sb_pool_scratch_ints(n)
         if ints == 0:
             raise ValueError("a pool has 1 .. 2^20 pages")
-        self.scratch = torch.empty(ints, dtype=i32, device=dev)
+        self._scratch = _Scratch(ints, i32, dev)
+        self.scratch = self._scratch.t
         self.c = B.Pool(
             _tensor(page_table, "page_table", i32, (shape.max_seqs, shape.max_pages)),
             _tensor(held, "held", i32, (shape.max_seqs,), dev),
@@ -269,8 +287,10 @@ class PagePool:
         _call(self.device, self.lib.sb_pool_fork, self.shape.c, self.c, n, pa, ch,
               _tensor(length, "length", torch.int32, (self.shape.max_seqs,),
                       self.device), self._kv, self._kvq)
+        self._scratch.used()
 
     def compact(self):
         """Moves the pages in use to the front of the pool."""
         _call(self.device, self.lib.sb_pool_compact, self.shape.c, self.c,
               self._kv, self._kvq)
+        self._scratch.used()
