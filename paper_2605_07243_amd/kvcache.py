@@ -196,6 +196,10 @@ class Attention:
         """Attention outputs of the rows, [n_rows][n_heads][head_dim]."""
         if not 0 <= layer < self._layers:
             raise ValueError(f"layer must be in 0 .. {self._layers - 1}")
+        if (q.requires_grad or (out is not None and out.requires_grad)
+                ) and torch.is_grad_enabled():
+            raise ValueError("attention over the 8-bit cache has no backward pass: "
+                             "call it under torch.no_grad() or on q.detach()")
         if out is None:
             out = torch.empty_like(q)
         if not (self._fits(q) and self._fits(out)):
