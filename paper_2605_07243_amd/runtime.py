@@ -284,6 +284,7 @@ class Runtime:
         self.draft_kv = kvcache.PagedKV(shape, self.dk, self.dv, self.dpt)
         self.tkv_c, self.dkv_c = self.staging.c, self.draft_kv.c
         self.kvq = kvcache.QuantKV.empty(shape, s.n_layers, n_pages, self.tpt)
+        self._upto = torch.zeros_like(self.T)   # (a commit's lengths, but one)
         self.pool.attach([self.draft_kv, self.kvq])
 
     # ------------------------------------------------------------------
@@ -386,8 +387,9 @@ class Runtime:
                          C.c_void_p(0))
         if self.kvq is not None:
             self._staged = None
-            # pages for what this commit may add
-            self.pool.grow(self.T, self.w.M * self.w.K + 1)
+            # pages for what this commit adds: the root and the accepted nodes
+            torch.add(self.T, self.aout["n_accepted"], out=self._upto)
+            self.pool.grow(self._upto, 1)
             self._check(self.lib.sb_commit_kvq(
                 self.ctx, C.byref(self.seqs_c), C.byref(self.tree_c),
                 C.byref(vc), C.byref(self.aout_c), C.byref(self.kvq.c),
