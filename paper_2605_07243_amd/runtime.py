@@ -46,8 +46,9 @@ class Runtime:
     prefill_rows: prompt rows that a prefill pass may take (the workspace is
     sized for them; prefill_chunk is the least).
     kvq: the target's committed K/V in 8 bits, pages of both models from one
-    pool (``self.kvq``, ``self.pool``): prefill fills the element-type cache
-    and stores it, verify, commit and fork use the 8-bit one.  window, sinks:
+    pool (``self.kvq``, ``self.pool``): prefill fills an element-type cache of
+    its prompts' pages and stores it, verify, commit and fork use the 8-bit
+    one; the first commit or fork lets the prompts' pages go.  window, sinks:
     what the verification sees of a long prefix (0, 0: all of it).
     """
 
@@ -102,7 +103,7 @@ class Runtime:
             ctx, C.byref(self.tw_c), C.byref(self.dw_c),
             _ptr(self.workspace), nbytes))
         self.kvq = self.pool = None
-        self._buffers(page_seed)
+        self._buffers(page_seed, kvq)
         if kvq:
             self._quantised()
 
@@ -204,7 +205,7 @@ class Runtime:
                 torch.int32)
         return m.to(self.dev).contiguous()
 
-    def _buffers(self, page_seed):
+    def _buffers(self, page_seed, kvq):
         w, s, dev, S = self.w, self.w.target, self.dev, self.S
         i32 = dict(dtype=torch.int32, device=dev)
         f32 = dict(dtype=torch.float32, device=dev)
@@ -222,10 +223,11 @@ class Runtime:
                 np.int32).reshape(S, self.max_pages)).to(dev)
             return k, v, pt
 
-        self.tk, self.tv, self.tpt = pool(s.n_layers)
+        if not kvq:
+            self.tk, self.tv, self.tpt = pool(s.n_layers)
+            self.tkv_c = B.KV(_ptr(self.tk), _ptr(self.tv), _ptr(self.tpt),
+                              s.n_layers, n_pages)
         self.dk, self.dv, self.dpt = pool(w.drafter_layers)
-        self.tkv_c = B.KV(_ptr(self.tk), _ptr(self.tv), _ptr(self.tpt),
-                          s.n_layers, n_pages)
         self.dkv_c = B.KV(_ptr(self.dk), _ptr(self.dv), _ptr(self.dpt),
                           w.drafter_layers, n_pages)
         self.root = torch.zeros(S, **i32)
@@ -270,22 +272,37 @@ class Runtime:
         self.V = V
 
     def _quantised(self):
-        """The 8-bit target cache, one page table and pool for it and the
-        drafter's cache, and the element-type cache that prefill fills, through
-        a table of its own (forks and compactions pass it by)."""
+        """The 8-bit target cache, and one page table and pool for it and the
+        drafter's cache."""
         s, w = self.w.target, self.w
         shape = kvcache.Shape(s.n_heads, s.n_kv_heads, s.head_dim, w.dtype,
                               self.S, self.max_pages)
-        n_pages = self.tk.shape[1]
-        self.pool = kvcache.PagePool.empty(shape, n_pages, self.tk.device)
-        self.staging = kvcache.PagedKV(shape, self.tk, self.tv, self.tpt)
-        self._staged = None     # prompt lengths, while it holds the cache's entries
+        n_pages = self.dk.shape[1]
+        self.pool = kvcache.PagePool.empty(shape, n_pages, self.dk.device)
         self.tpt = self.dpt = self.pool.page_table
         self.draft_kv = kvcache.PagedKV(shape, self.dk, self.dv, self.dpt)
-        self.tkv_c, self.dkv_c = self.staging.c, self.draft_kv.c
+        self.dkv_c = self.draft_kv.c
         self.kvq = kvcache.QuantKV.empty(shape, s.n_layers, n_pages, self.tpt)
         self._upto = torch.zeros_like(self.T)   # (a commit's lengths, but one)
         self.pool.attach([self.draft_kv, self.kvq])
+        # a prefill's element-type cache and its prompts' lengths, until the
+        # first commit or fork
+        self.staging = self._staged = None
+
+    def _stage(self, lens):
+        """An element-type cache of the pages of prompts of these lengths, with
+        a table of its own (forks and compactions pass it by)."""
+        s, shape = self.w.target, self.kvq.shape
+        table = np.full((self.S, self.max_pages), -1, np.int32)
+        n = 0
+        for row, length in zip(table, lens):
+            m = min((length + 15) // 16, self.max_pages)
+            row[:m] = np.arange(n, n + m)
+            n += m
+        z = lambda *d: torch.zeros(s.n_layers, max(n, 1), s.n_kv_heads, *d,  # noqa: E731
+                                   dtype=self.et, device=self.dev)
+        return kvcache.PagedKV(shape, z(16, s.head_dim), z(s.head_dim, 16),
+                               torch.from_numpy(table).to(self.dev))
 
     # ------------------------------------------------------------------
     @property
@@ -310,16 +327,18 @@ class Runtime:
             state = [(t, t.clone()) for t in (p.page_table, p.held, p.refs, p.refused)]
             p.reset()
             p.grow(dlens)
+            staging = self._stage(lens)
+        tkv_c = self.tkv_c if self.kvq is None else staging.c
         rc = self.lib.sb_prefill(
             self.ctx, C.byref(self.seqs_c), _ptr(self.prompt_dev), ld, clens,
-            C.byref(self.tkv_c), C.byref(self.dkv_c), self.stream)
+            C.byref(tkv_c), C.byref(self.dkv_c), self.stream)
         if self.kvq is not None and rc != B.SB_OK:
             for t, was in state:
                 t.copy_(was)
         self._check(rc)
         if self.kvq is not None:
-            self.kvq.store(self.staging, torch.zeros_like(dlens), dlens, ld)
-            self._staged = lens
+            self.kvq.store(staging, torch.zeros_like(dlens), dlens, ld)
+            self.staging, self._staged = staging, lens
 
     def expand(self, m, want_logits=False):
         if want_logits:
@@ -386,7 +405,7 @@ class Runtime:
         vc = B.VerifyOut(_ptr(self.vout["argmax"]), _ptr(self.vout["taps"]),
                          C.c_void_p(0))
         if self.kvq is not None:
-            self._staged = None
+            self.staging = self._staged = None
             # pages for what this commit adds: the root and the accepted nodes
             torch.add(self.T, self.aout["n_accepted"], out=self._upto)
             self.pool.grow(self._upto, 1)
@@ -413,7 +432,7 @@ class Runtime:
         if self.pool is None:
             raise ValueError("forks need the 8-bit cache (kvq)")
         self.pool.fork(parents, children, self.T)
-        self._staged = None
+        self.staging = self._staged = None
         a = torch.tensor(list(parents), device=self.dev)
         b = torch.tensor(list(children), device=self.dev)
         for t in (self.root, self.T, self.cond_taps):
@@ -539,13 +558,14 @@ class Runtime:
         cache holds."""
         if which == "target8":
             return self._read_cache8(seq, n, start)
-        K_, V_, pt = self._pool(which)
         if which == "target" and self.kvq is not None:
             if self._staged is None or start + n > self._staged[seq]:
                 raise ValueError(
                     "the element-type cache holds a prefill's entries until the "
                     'first commit or fork: read "target8"')
-            pt = self.staging.page_table
+            K_, V_, pt = self.staging.k, self.staging.v, self.staging.page_table
+        else:
+            K_, V_, pt = self._pool(which)
         pages, slots = self._slots(pt, seq, n, start)
         ks = torch.stack([K_[layer][pages, :, slots, :]
                           for layer in range(K_.shape[0])])
