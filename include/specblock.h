@@ -583,7 +583,8 @@ typedef struct sb_kvq {
  * |x| <= 448 * 2^e for every finite value x stored by this call; when the page
  * holds earlier entries (below first) its exponent does not fall, and where it
  * rises the held codes are rounded again to the new one (exactly, but for
- * values below the least normal code).  A code is x * 2^-e rounded to nearest,
+ * values below the least normal code: a held value stays within 2^-4 |x| +
+ * 2^-9 2^e of what was stored).  A code is x * 2^-e rounded to nearest,
  * ties to even; infinities and NaN become NaN.  Other slots keep their bytes.
  * Sequences must not share the pages written.  The layer counts must agree.
  * Errors: SB_EINVAL, SB_ESHAPE, SB_EDTYPE, SB_EHIP. */
@@ -602,7 +603,8 @@ typedef struct sb_attn_rows {
                                   rows of a sequence past it are not computed */
   int32_t max_prefix;          /* host bound of prefix_len; 0: the page
                                   table's capacity.  Entries past it are not
-                                  seen                                       */
+                                  seen.  It sets how the work is split: one
+                                  far above the lengths costs time           */
   int32_t vis_words;           /* host: words per row of vis, 0..16          */
   int32_t seg_pages;           /* host: segment pages per sequence; 0: none  */
   const int32_t* row_off;      /* [n_seqs + 1], ascending                    */
@@ -628,7 +630,9 @@ size_t sb_kvq_attend_workspace(const sb_cache_shape* shape,
  * nothing, whatever they hold.  window > 0: row i sees entry e only when
  * e < sinks or e > pos[i] - window (its own window and the first `sinks`
  * entries, which stay visible); the segment is not windowed.  window 0: the
- * whole prefix.
+ * whole prefix.  Scores, statistics and sums are fp32; with SB_BF16 each
+ * probability is rounded to bf16 for its product with v_e (not in the sum
+ * that it is divided by), and the output once.
  * q, out: elem [n_rows][n_heads][head_dim], 16-byte aligned, not overlapping;
  * rows outside row_off's range are left as they were.
  * workspace: device, 256-byte aligned, of sb_kvq_attend_workspace bytes, used
@@ -693,8 +697,9 @@ int sb_pool_release(const sb_cache_shape* shape, const sb_pool* pool, int32_t n,
  * pages below len[parent] (device [max_seqs], cut to what the parent holds)
  * and gets a copy of its last, partly filled one in the lowest free page (in
  * order of i; refused counts a child that finds none: it holds the full pages
- * only, and its length is the caller's to cut to them).  kv, kvq: the caches whose pages are copied (either may be NULL),
- * with the pool's page table and page count. */
+ * only, and its length is the caller's to cut to them).  kv, kvq: the caches
+ * whose pages are copied (either may be NULL), with the pool's page table and
+ * page count. */
 int sb_pool_fork(const sb_cache_shape* shape, const sb_pool* pool, int32_t n,
                  const int32_t* parent, const int32_t* child,
                  const int32_t* len, const sb_kv* kv, const sb_kvq* kvq,

@@ -24,10 +24,11 @@
 // its sum is taken before the rounding, in fp32.
 //
 // What bounds it.  Single tokens: the codes' way from HBM (64 sequences of 4096
-// to 32768 entries: 2.4 GB in 418-455 us, 5.3 to 5.8 TB/s; a streaming read
+// to 32768 entries: 2.4 GB in 413-460 us, 5.3 to 5.9 TB/s; a streaming read
 // reaches 6.8).  Trees: every 32 query vectors read all of their KV head's codes from
-// L2 and convert them; 500 rows over 8192 entries take 90 us (640 TFLOP/s; 70
-// without the loads, 49 for the products alone at a large bf16 product's rate).
+// L2 and convert them; 500 rows over 8192 entries take 89-95 us (630 TFLOP/s; 49
+// for the products alone at a large bf16 product's rate), in which a SIMD's vector
+// instructions take 62% of the cycles and its matrix instructions 35%.
 // Short prefixes: launch and the chain row bounds -> page table -> codes (a row
 // over 1024 entries 9.4 us, of which an empty launch is 5).
 #include <hip/hip_ext.h>
@@ -364,7 +365,7 @@ __global__ __launch_bounds__(256, 2) void kvq_attn_kernel(
       f32x4_t sc[2];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-sc[h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        sc[h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
         const uint32_t* w = reinterpret_cast<const uint32_t*>(&kd[h][0]);
 #pragma unroll
         for (int i = 0; i < NK; ++i) {
@@ -565,10 +566,10 @@ sc[h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 // A workgroup: 32 query vectors of one KV head, one split; its NW waves take
 // every NW-th tile, as above.  Two waves a SIMD (the accumulators, the queries
 // and two tiles of loads fill the registers).  Bound inside the CU: the same 500
-// rows take 90 us, 48 with the loads alone and 70 without them.  Measured beside it:
-// 16 query vectors a wave 171, 64 a wave 94 to 108, four waves of other queries on
-// the same tiles 118, tiles converted once for four such waves and shared in LDS
-// 101.
+// rows took 90 us, 48 with the loads alone and 70 without them.  Measured while K
+// came straight into the operand's registers (93 us then): 64 query vectors a wave 94
+// to 108, four waves of other queries on the same tiles 104 to 120, tiles converted
+// once for four such waves and shared in LDS 101.
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
@@ -1052,17 +1053,20 @@ int cdiv(long a, long b) { return (int)((a + b - 1) / b); }
 }  // namespace
 
 // 32 query vectors a workgroup where there are more than 16 of a KV head (16
-// trees of up to 64 nodes 68 us with 16, 48 with 32; fp32 has 16 throughout).
+// trees of up to 64 nodes 71 us with 16, 46 with 32; fp32 has 16 throughout).
 // No split below 1280 entries, where the merge costs what it saves (a row over
-// 512: 7.2 us, in two 9.4; 60 nodes over 1024: 12.4, in four 13.2; over 1536:
-// 14.9, in six 13.6).  Beyond that as many as give a workgroup on every CU and
-// keep 256 entries each, of more than eight 512 (a row over 8192: 14.0 us in 16,
-// 16.6 in 32): what a second one on a CU gains the merge costs (500 rows over
-// 8192: 94 us, in two 106; 8 windows of 4096, 33 rows each: 30.5, in two 38.7).
+// 512: 7.5 us, in two 10.0; 60 nodes over 1024: 12.0, in four 13.2; over 1536:
+// 14.3, in four 13.7).  Beyond that as many as give a workgroup on every CU and
+// keep 256 entries each, of more than eight 512 (a row over 8192: 13.0 us in 16,
+// 15.3 in 32): what a second one on a CU gains the merge costs (500 rows over
+// 8192: 94 us, in two 105; 8 windows of 4096, 33 rows each: 29.6, in two 34.5).
 // Longer prefixes are cut to 8192 entries so that ragged batches end together.
+// The bound stands in for the lengths, which only the device knows: 60 rows over
+// 8192 take 23 us with a bound of 8192, 43 with 32768, 50 with 262144.
 // Eight waves a workgroup where there is at most one on a CU and it has 1024
-// entries (8 windows of 4096: 28.8 us, with four 31.7; 60 nodes over 16384: 31.7
-// and 33.3; with splits of 256 or 512 entries four are 2 to 6% faster).
+// entries (8 windows of 4096: 29.6 us, with four 32.1; 60 nodes over 16384: 31.9
+// and 33.4; with splits of 256 or 512 entries four are 1 to 4% faster, with two
+// workgroups on a CU 20%).
 QPlan kvq_attn_plan(int n_seqs, int rows_per_seq, int max_prefix, int window,
                     int sinks, int H, int Hkv, int es, int max_split) {
   long eff = max_prefix;

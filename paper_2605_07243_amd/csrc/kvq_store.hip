@@ -5,16 +5,18 @@
 // values.  It finds the largest finite |x| of the entries that it stores,
 // takes the least exponent e with |x| <= 448 2^e (bit arithmetic on the fp32
 // value: 448 = 1.75 * 2^8), at least the page's own where it holds earlier
-// entries, and writes x 2^-e as e4m3, ties to even; held codes follow a risen
-// exponent.  The products with powers of two are exact, so a value is rounded
-// once, whoever computes it.
+// entries, and writes x 2^-e as e4m3, ties to even.  The products with powers of
+// two are exact, so the call rounds a value once.  Held codes follow a risen
+// exponent: those that stay at or above the least normal code exactly, the others
+// rounded to the new scale's 2^-9 2^e steps; over any number of rises a held value
+// is within 2^-4 |x| + 2^-9 2^e of what was stored.
 //
 // HBM bound: es + 1 bytes per value.  The loads of a wave cover whole
 // contiguous runs (K: 1 KiB per instruction; V: lane (a, r) reads slots 4 a ..
 // 4 a + 3 of column 16 c + r, 512 B per instruction for bf16), and V's stores
 // are hd / 4 consecutive bytes a lane.  16 prompts of 512 to 2048 entries in 8
 // layers of 8 x 128 heads: 183-208 us, 4.8 to 5.5 TB/s.  The few entries of one
-// iteration (16 sequences, 32 layers) take 12.8 us: a launch and the chain
+// iteration (16 sequences, 32 layers) take 13 us: a launch and the chain
 // bounds -> page -> scale and codes, each step a trip to memory.
 #include <algorithm>
 

@@ -10,8 +10,8 @@
 // no order.
 //
 // The bookkeeping is a few launches of a few microseconds (15 forks of a prompt
-// of 1003 entries in 32 layers: 17.4 us, of which the three launches are 10 and
-// the copy of 15.7 MB 7); copies run at the rate of a plain copy.
+// of 1003 entries in 32 layers: kernels of 2.4 and 4.0 us, and the copy of 15.7 MB
+// 5.4); copies run at the rate of a plain copy.
 #include <algorithm>
 
 #include "bounds.h"

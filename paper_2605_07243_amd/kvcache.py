@@ -146,7 +146,9 @@ class Attention:
     """sb_kvq_attend for one description of rows (sb_attn_rows) and one
     workspace: ``plan(layer, q, out)`` for every layer of a forward.  A plan
     runs on one stream at a time; captured graphs that may run at the same
-    time need a plan each, which has to live as long as its graph."""
+    time need a plan each, which has to live as long as its graph.
+    max_prefix bounds prefix_len (0: the page table's capacity) and sets how
+    the work is split: the nearer to the lengths, the faster."""
 
     def __init__(self, cache, row_off, pos, prefix_len, seg_len=None, vis=None,
                  seg_k=None, seg_v=None, *, n_rows, rows_per_seq, max_prefix=0,

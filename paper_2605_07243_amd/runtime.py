@@ -428,7 +428,8 @@ class Runtime:
 
     def fork(self, parents, children):
         """Sequences children[i] become continuations of parents[i] from their
-        present state (kvq only): full pages shared, the last one copied."""
+        committed state (kvq only): full pages shared, the last one copied.
+        Between a commit and the next expand: a tree is not copied."""
         if self.pool is None:
             raise ValueError("forks need the 8-bit cache (kvq)")
         self.pool.fork(parents, children, self.T)
