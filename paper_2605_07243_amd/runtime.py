@@ -322,12 +322,13 @@ class Runtime:
         clens = (C.c_int32 * self.S)(*lens)
         if self.kvq is not None:
             dlens = torch.tensor(lens, dtype=torch.int32).to(self.dev)
-            # (prompts that the library refuses leave the sequences as they are)
+            # (prompts that the library refuses, or that memory does not hold,
+            # leave the sequences as they are)
+            staging = self._stage(lens)
             p = self.pool
             state = [(t, t.clone()) for t in (p.page_table, p.held, p.refs, p.refused)]
             p.reset()
             p.grow(dlens)
-            staging = self._stage(lens)
         tkv_c = self.tkv_c if self.kvq is None else staging.c
         rc = self.lib.sb_prefill(
             self.ctx, C.byref(self.seqs_c), _ptr(self.prompt_dev), ld, clens,

@@ -73,3 +73,23 @@ def test_prompts_that_fill_their_tables(dtype):
                         <= 2.0 ** -4 * np.abs(a) + 2.0 ** -17 * top).all()
         rt.iteration()
     assert int(rt.pool.refused[0]) == 0
+
+
+def test_prompts_that_memory_does_not_hold():
+    """An allocation that fails in a prefill leaves the sequences their pages."""
+    w = workload("bf16", 2, 40, 30)
+    weights, _, _ = models(w)
+    rt = runtime(w, weights, max_pages=10, kvq=True)
+    rt.prefill(synth.prompts(w))
+    rt.iteration()
+    state = [host(t).copy() for t in (rt.pool.page_table, rt.pool.held, rt.pool.refs, rt.T)]
+
+    def no_room(lens):
+        raise torch.OutOfMemoryError("no room")
+
+    stage, rt._stage = rt._stage, no_room
+    with pytest.raises(torch.OutOfMemoryError):
+        rt.prefill(synth.prompts(w))
+    rt._stage = stage
+    for t, was in zip((rt.pool.page_table, rt.pool.held, rt.pool.refs, rt.T), state):
+        np.testing.assert_array_equal(host(t), was)
